@@ -64,7 +64,8 @@ typedef enum fc_kind {
   FC_FORCE    = 9   /* identity; every edge out of it is infusible */
 } fc_kind;
 
-typedef enum fc_dtype { FC_F32 = 0, FC_I32 = 1 } fc_dtype;
+/* Programs are made of the first two; the others are element types of the operators' arrays (below). */
+typedef enum fc_dtype { FC_F32 = 0, FC_I32 = 1, FC_F16 = 2, FC_BF16 = 3, FC_I64 = 4 } fc_dtype;
 
 /* Element functions (the paper allows arbitrary lambdas; the kernels here are
  * hand written, so the lambdas form a closed vocabulary). */
@@ -288,6 +289,143 @@ int fc_bind(const fc_graph *g, const fc_partition *p, const fc_buffer *bufs, voi
             fc_bound **out);
 int fc_run_bound(const fc_bound *b, void *hip_stream);
 int fc_unbind(fc_bound *b);
+
+/* ---------------------------------------------------------------- operators of a serving cache */
+/* The pattern of this library -- index arrays decide what a reduction reads and a scatter writes, and nothing in between
+ * reaches memory -- at the place where language models meet it: a cache of keys and values in pages.  FC_PAGE_MAP scans the
+ * requests' lengths into block tables and slot maps, FC_HEAD_NORM_ROPE writes keys and values through the slot map,
+ * FC_PAGED_ATTENTION folds over the cache gathered through the block table.  The language above cannot say them (rank 2,
+ * 32-bit elements, a closed vocabulary), so each is an operator of its own.
+ *
+ * An operator is a kind and a struct of its arrays.  Lists of operators run in order on a stream under the rules of programs:
+ * fc_run_operators enqueues and returns; fc_bind_operators does the host's work once, for callers that run the
+ * same operators on the same arrays step after step (the bound list is an fc_bound: fc_run_bound, fc_unbind); nothing is
+ * allocated, nothing synchronises, no memset or copy is enqueued, so a step can be captured into a graph.  Scratch is that of
+ * fc_run_fused: 256-byte aligned, its first FC_SCRATCH_CONTROL_BYTES zero the first time, not shared by calls that overlap in time.
+ *
+ * Shapes, types, strides and alignment are checked before anything is enqueued (FC_E_ARG: wrong, FC_E_UNSUPPORTED: right but not
+ * built, FC_E_UNBOUND: no memory or misaligned, FC_E_LIMIT: an extent beyond 2^31-1).  What lies in device memory cannot be: lengths,
+ * page numbers, slots and positions out of range are defined below, and no kernel reads or writes outside its arrays for
+ * them.  Outputs must not overlap inputs or each other except where it is said. */
+
+/* A DEVICE array.  rank 0: absent.  Strides in elements; the innermost is 1, and those of an array that is written keep its
+ * elements apart.  ptr is aligned to the element, and may be NULL where an extent is 0. */
+typedef struct fc_tensor {
+  void   *ptr;
+  int32_t dtype;      /* fc_dtype */
+  int32_t rank;       /* 0 to 4 */
+  int64_t shape[4];
+  int64_t stride[4];
+} fc_tensor;
+
+typedef enum fc_operator_kind {
+  FC_PAGE_MAP            = 0,  /* args: fc_page_map            */
+  FC_HEAD_NORM_ROPE      = 1,  /* args: fc_head_norm_rope      */
+  FC_HEAD_NORM_ROPE_GRAD = 2,  /* args: fc_head_norm_rope_grad */
+  FC_PAGED_ATTENTION     = 3   /* args: fc_paged_attention     */
+} fc_operator_kind;
+
+typedef struct fc_operator {
+  int32_t     kind;
+  const void *args;
+} fc_operator;
+
+/* Block table and slot map of one step of a server.  B requests, tables of W pages each, pages of P = page_size tokens, a ring of
+ * C page numbers that holds the free pages from cursor[0] (taken from there) up to cursor[1] (given back there), both counting on
+ * for ever, C at least the number of pages.  new_tokens[r] > 0: tokens request r adds in this step; < 0: tokens it drops from its
+ * end (-lengths[r]: it leaves).  With pages(n) = min(ceil(n / P), W), len = max(lengths[r], 0), want = max(len + new_tokens[r], 0):
+ *   the pages pages(len) .. pages(want)-1 are taken from the ring, requests in order, and entered in the table; where the ring
+ *   runs out the rest stay as they are, and the request keeps the tokens that fit: lengths_after[r] = want, or the least of want
+ *   and what its pages hold.  The pages pages(want) .. pages(len)-1 of a request that shrinks go to the ring, requests in order;
+ *   pages given back are not taken in the same step.
+ *   row_start[r] = number of new tokens of the requests before r.  Token t of the step, j-th new token of request r:
+ *   request[t] = r, positions[t] = len + j, slots[t] = table[r][positions[t] / P] * P + positions[t] mod P, or -1 if it has no place
+ *   (positions[t] >= lengths_after[r], or its entry is negative).  Past the last token: -1, 0, -1.
+ *   cursor_after: the cursor of the next step; unplaced[0]: tokens of all requests that found no page.
+ * cursor, lengths and new_tokens are not written, so a step that is run again gives the same; the ring and the table
+ * are written in place.  Tokens beyond the extent of slots have no entry. */
+typedef struct fc_page_map {
+  int32_t   page_size;
+  fc_tensor lengths;        /* i32 [B] */
+  fc_tensor new_tokens;     /* i32 [B] */
+  fc_tensor pool;           /* i32 [C], in and out */
+  fc_tensor cursor;         /* i64 [2] */
+  fc_tensor table;          /* i32 [B, W], in and out */
+  fc_tensor lengths_after;  /* i32 [B], out */
+  fc_tensor row_start;      /* i32 [B + 1], out */
+  fc_tensor slots;          /* i64 [T], out */
+  fc_tensor positions;      /* i32 [T], out */
+  fc_tensor request;        /* i32 [T], out */
+  fc_tensor cursor_after;   /* i64 [2], out */
+  fc_tensor unplaced;       /* i64 [1], out */
+} fc_page_map;
+
+/* Norm of every query and key head and rotation by position, in one pass.  x, one head of one token, D elements:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight   (y = x where the weight is absent),
+ *   the first R elements of y are turned in pairs, the i-th pair, i < R/2, by the angle whose cosine and sine are cos_sin[p][i] and
+ *   cos_sin[p][R/2 + i], p = positions[axis_of[i]][t] (axis 0 where axis_of is absent; no rotation where cos_sin is); a pair is
+ *   (y[i], y[i + R/2]), interleaved: (y[2i], y[2i + 1]);  (a, b) -> (a c - b s, b c + a s).
+ * In 32 bits, rounded once.  Keys go to k_out, or, with values as they are, to row slots[t] of the caches (page slots[t] / P, place
+ * slots[t] mod P); slots outside the cache, -1 among them, are skipped; slots of one call are distinct.  A position or an axis outside
+ * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides). */
+typedef struct fc_head_norm_rope {
+  fc_tensor q;            /* [T, Hq, D]: f32, f16 or bf16; D <= 512 */
+  fc_tensor k;            /* [T, Hk, D] */
+  fc_tensor q_weight;     /* [D] of the same type, or absent */
+  fc_tensor k_weight;
+  fc_tensor cos_sin;      /* f32 [positions there are, R], R even, R <= D; or absent */
+  fc_tensor positions;    /* i32 [axes, T]; absent with cos_sin */
+  fc_tensor axis_of;      /* i32 [R / 2], or absent */
+  fc_tensor q_out;        /* [T, Hq, D], out */
+  fc_tensor k_out;        /* [T, Hk, D], out; absent with slots */
+  fc_tensor v;            /* [T, Hk, D]; with slots */
+  fc_tensor k_cache;      /* [pages, P, Hk, D], out; with slots */
+  fc_tensor v_cache;
+  fc_tensor slots;        /* i64 [T], or absent */
+  double    eps;
+  int32_t   interleaved;
+} fc_head_norm_rope;
+
+/* Its gradient: dq and dk from the gradients of q_out and k_out, and (f32) those of the weights, summed over tokens and heads in a
+ * fixed order.  With g = dy turned back, u = x * rsqrt(mean(x^2) + eps): dweight = sum g u, dx = rsqrt(...) * (w g - u mean(w g u)).
+ * dq may be dq_out and dk may be dk_out. */
+typedef struct fc_head_norm_rope_grad {
+  fc_tensor q, k, q_weight, k_weight, cos_sin, positions, axis_of;   /* as above */
+  fc_tensor dq_out;       /* [T, Hq, D] */
+  fc_tensor dk_out;       /* [T, Hk, D] */
+  fc_tensor dq;           /* [T, Hq, D], out */
+  fc_tensor dk;           /* [T, Hk, D], out */
+  fc_tensor dq_weight;    /* f32 [D], out; absent with q_weight */
+  fc_tensor dk_weight;    /* f32 [D], out; absent with k_weight */
+  double    eps;
+  int32_t   interleaved;
+} fc_head_norm_rope_grad;
+
+/* Attention of one new token of each request over its pages of the cache.  Request b sees the keys j of
+ * [max(0, len - window), len), len = lengths[b] (window 0: all), at place j mod P of page table[b][j / P]; keys on pages that are
+ * outside the cache or the table are not there.  Query head h reads key head h / (Hq / Hk).
+ *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
+ * A request without keys gets zeros and -inf.  What lies in the pages past a request's length is not looked at, whatever it holds. */
+typedef struct fc_paged_attention {
+  fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256 */
+  fc_tensor k_cache;      /* [pages, P, Hk, D], in any order of strides with D innermost; rows 16-byte aligned */
+  fc_tensor v_cache;
+  fc_tensor table;        /* i32 [B, W] */
+  fc_tensor lengths;      /* i32 [B] */
+  fc_tensor out;          /* [B, Hq, D], out */
+  fc_tensor lse;          /* f32 [B, Hq], out, or absent */
+  double    scale;
+  int32_t   window;
+} fc_paged_attention;
+
+/* Bytes of scratch a list of operators needs. */
+int fc_operators_scratch_bytes(const fc_operator *ops, int32_t n, size_t *bytes);
+
+/* Enqueue the operators in order on `hip_stream`. */
+int fc_run_operators(const fc_operator *ops, int32_t n, void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* The same in two halves, as fc_bind: *out is run by fc_run_bound and released by fc_unbind. */
+int fc_bind_operators(const fc_operator *ops, int32_t n, void *scratch, size_t scratch_bytes, fc_bound **out);
 
 /* Status of the device work enqueued so far by fc_run_* calls that used `scratch`.
  *

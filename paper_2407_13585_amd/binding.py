@@ -56,7 +56,7 @@ FC_SCRATCH_CONTROL_BYTES = 1 << 23
 
 KIND = {"input": 0, "map": 1, "generate": 2, "gather": 3, "fold": 4, "foldseg": 5,
         "scanl": 6, "scanr": 7, "scatter": 8, "force": 9}
-DTYPE = {"f32": 0, "i32": 1}
+DTYPE = {"f32": 0, "i32": 1, "f16": 2, "bf16": 3, "i64": 4}
 FN = {"": 0, "ident": 1, "affine": 2, "sin_x_mul_x": 3, "sq_plus_one": 4, "mul2": 5, "add2": 6,
       "add3": 7, "add5": 8, "exp_neg": 9, "mod_eq": 10,
       "iota": 32, "iota_rev": 33, "clamp_shift_2d": 34, "row_of_2d": 35, "const_i32": 36}
@@ -100,6 +100,37 @@ class fc_partition(C.Structure):
 
 class fc_buffer(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("bytes", C.c_int64)]
+
+
+class fc_tensor(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("rank", C.c_int32), ("shape", C.c_int64 * 4), ("stride", C.c_int64 * 4)]
+
+
+class fc_operator(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("args", C.c_void_p)]
+
+
+def _tensors(*names):
+    return [(n, fc_tensor) for n in names]
+
+
+class fc_page_map(C.Structure):
+    _fields_ = [("page_size", C.c_int32)] + _tensors("lengths", "new_tokens", "pool", "cursor", "table", "lengths_after", "row_start", "slots",
+                                                     "positions", "request", "cursor_after", "unplaced")
+
+
+class fc_head_norm_rope(C.Structure):
+    _fields_ = _tensors("q", "k", "q_weight", "k_weight", "cos_sin", "positions", "axis_of", "q_out", "k_out", "v", "k_cache", "v_cache",
+                        "slots") + [("eps", C.c_double), ("interleaved", C.c_int32)]
+
+
+class fc_head_norm_rope_grad(C.Structure):
+    _fields_ = _tensors("q", "k", "q_weight", "k_weight", "cos_sin", "positions", "axis_of", "dq_out", "dk_out", "dq", "dk", "dq_weight",
+                        "dk_weight") + [("eps", C.c_double), ("interleaved", C.c_int32)]
+
+
+class fc_paged_attention(C.Structure):
+    _fields_ = _tensors("q", "k_cache", "v_cache", "table", "lengths", "out", "lse") + [("scale", C.c_double), ("window", C.c_int32)]
 
 
 _lib = None
@@ -149,7 +180,11 @@ def lib() -> C.CDLL:
     L.fc_unbind.argtypes = [C.c_void_p]
     L.fc_check.argtypes = [C.c_void_p, C.c_void_p]
     L.fc_run_fused_static.argtypes = [PG, PP, C.POINTER(fc_buffer), C.c_void_p]
-    for f in ("fc_bind", "fc_run_bound", "fc_unbind", "fc_check", "fc_run_fused_static", "fc_num_edges", "fc_plan", "fc_plan_weighted", "fc_plan_greedy", "fc_partition_trivial", "fc_partition_check", "fc_duplicate",
+    PO = C.POINTER(fc_operator)
+    L.fc_operators_scratch_bytes.argtypes = [PO, C.c_int32, C.POINTER(C.c_size_t)]
+    L.fc_run_operators.argtypes = [PO, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.fc_bind_operators.argtypes = [PO, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(C.c_void_p)]
+    for f in ("fc_operators_scratch_bytes", "fc_run_operators", "fc_bind_operators", "fc_bind", "fc_run_bound", "fc_unbind", "fc_check", "fc_run_fused_static", "fc_num_edges", "fc_plan", "fc_plan_weighted", "fc_plan_greedy", "fc_partition_trivial", "fc_partition_check", "fc_duplicate",
               "fc_scratch_bytes", "fc_run_fused", "fc_run_unfused", "fc_cluster_kernel"):
         getattr(L, f).restype = C.c_int
     _run_bound_address = C.cast(L.fc_run_bound, C.c_void_p).value
@@ -457,6 +492,129 @@ class BoundRun(_Bound):
         else:
             rc = self._lib.fc_run_fused(self._g.ref(), C.byref(self._cp), self._bufs, self._sp, self._sb,
                                         stream or None)
+        self._failed(rc)
+
+    def _failed(self, rc: int) -> None:
+        if rc != 0:
+            _check(rc)
+
+
+# ------------------------------------------------------------------ operators of a serving cache
+def _tensor(x) -> fc_tensor:
+    """A torch tensor on the device (the caller's; None: absent) as the struct of the ABI."""
+    t = fc_tensor()
+    if x is None:
+        return t
+    name = str(x.dtype).replace("torch.", "")
+    code = {"float32": "f32", "int32": "i32", "float16": "f16", "bfloat16": "bf16", "int64": "i64"}.get(name)
+    if code is None:
+        raise ValueError(f"tensors of type {name} are not taken")
+    if x.device.type != "cuda":
+        raise ValueError(f"tensors are in device memory, not on {x.device}")
+    if x.dim() < 1 or x.dim() > 4:
+        raise ValueError(f"tensors have 1 to 4 dimensions, not {x.dim()}")
+    t.ptr, t.dtype, t.rank = x.data_ptr() or None, DTYPE[code], x.dim()
+    t.shape[:t.rank], t.stride[:t.rank] = x.shape, x.stride()
+    return t
+
+
+class CacheOperator:
+    """One operator on the caller's tensors, which live as long as this object.  Every check is the library's."""
+
+    kind = -1
+    struct = None
+
+    def _describe(self, tensors: Dict[str, object], **scalars) -> None:
+        self.tensors = tensors
+        self.c = self.struct(**scalars)
+        for name, x in tensors.items():
+            setattr(self.c, name, _tensor(x))
+
+
+class PageMap(CacheOperator):
+    """Block table and slot map of a step from the requests' lengths: see fc_page_map in include/fc.h."""
+
+    kind, struct = 0, fc_page_map
+
+    def __init__(self, *, page_size: int, lengths, new_tokens, pool, cursor, table, lengths_after, row_start, slots, positions, request,
+                 cursor_after, unplaced):
+        self._describe(dict(lengths=lengths, new_tokens=new_tokens, pool=pool, cursor=cursor, table=table, lengths_after=lengths_after,
+                            row_start=row_start, slots=slots, positions=positions, request=request, cursor_after=cursor_after,
+                            unplaced=unplaced), page_size=page_size)
+
+
+class HeadNormRope(CacheOperator):
+    """Norm of query and key heads and rotation by position in one pass, keys (and values) to k_out or through `slots` into
+    the caches: see fc_head_norm_rope."""
+
+    kind, struct = 1, fc_head_norm_rope
+
+    def __init__(self, *, q, k, q_out, k_out=None, v=None, k_cache=None, v_cache=None, slots=None, q_weight=None, k_weight=None,
+                 eps: float = 1e-6, cos_sin=None, positions=None, axis_of=None, interleaved: bool = False):
+        self._describe(dict(q=q, k=k, q_out=q_out, k_out=k_out, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots, q_weight=q_weight,
+                            k_weight=k_weight, cos_sin=cos_sin, positions=positions, axis_of=axis_of), eps=eps, interleaved=int(interleaved))
+
+
+class HeadNormRopeGrad(CacheOperator):
+    """The gradient of HeadNormRope into tensors: see fc_head_norm_rope_grad."""
+
+    kind, struct = 2, fc_head_norm_rope_grad
+
+    def __init__(self, *, q, k, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 cos_sin=None, positions=None, axis_of=None, interleaved: bool = False):
+        self._describe(dict(q=q, k=k, dq_out=dq_out, dk_out=dk_out, dq=dq, dk=dk, dq_weight=dq_weight, dk_weight=dk_weight, q_weight=q_weight,
+                            k_weight=k_weight, cos_sin=cos_sin, positions=positions, axis_of=axis_of), eps=eps, interleaved=int(interleaved))
+
+
+class PagedAttention(CacheOperator):
+    """Attention of one new token of each request over its pages: see fc_paged_attention.  scale None: 1 / sqrt(D)."""
+
+    kind, struct = 3, fc_paged_attention
+
+    def __init__(self, *, q, k_cache, v_cache, table, lengths, out, lse=None, scale: Optional[float] = None, window: int = 0):
+        self._describe(dict(q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths, out=out, lse=lse),
+                       scale=q.shape[-1] ** -0.5 if scale is None else scale, window=window)
+
+
+def _operators(ops: Sequence[CacheOperator]):
+    arr = (fc_operator * max(len(ops), 1))()
+    for i, op in enumerate(ops):
+        arr[i].kind, arr[i].args = op.kind, C.addressof(op.c)
+    return arr
+
+
+def fc_operators_scratch_bytes(ops: Sequence[CacheOperator]) -> int:
+    b = C.c_size_t()
+    _check(lib().fc_operators_scratch_bytes(_operators(ops), len(ops), C.byref(b)))
+    return b.value
+
+
+def fc_run_operators(ops: Sequence[CacheOperator], scratch, stream: int = 0) -> None:
+    """Enqueues the operators in order on `stream` (a hipStream_t value); returns without synchronising."""
+    sp, sb = _scratch(scratch)
+    _check(lib().fc_run_operators(_operators(ops), len(ops), sp, sb, stream or None))
+
+
+class BoundOperators(_Bound):
+    """fc_run_operators with the host's work done once, for callers that run the same operators on the same tensors step after
+    step: `bound(stream=0)`.  What is wrong with the arguments is reported here."""
+
+    def __init__(self, ops: Sequence[CacheOperator], scratch):
+        ops = list(ops)
+        self._keep = (ops, scratch)                     # the device memory must outlive the calls
+        self._lib = lib()
+        sp, sb = _scratch(scratch)
+        handle = C.c_void_p()
+        _check(self._lib.fc_bind_operators(_operators(ops), len(ops), sp, sb, C.byref(handle)))
+        self._handle = _BoundHandle(self._lib, handle.value)
+        self._arm(self._handle, self._handle.value, _run_bound_address)
+
+    def __getstate__(self):                             # a copy shares the bound operators, and is armed by its first call
+        return self.__dict__
+
+    def _call(self, stream: int = 0) -> None:
+        rc = self._lib.fc_run_bound(self._handle.value, stream)
+        self._arm(self._handle, self._handle.value, _run_bound_address)
         self._failed(rc)
 
     def _failed(self, rc: int) -> None:

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "model.hpp"
+#include "operators.hpp"
 #include "plan.hpp"
 #include "run.hpp"
 
@@ -384,6 +385,45 @@ int fc_bind(const fc_graph *g, const fc_partition *p, const fc_buffer *bufs, voi
     int rc = run_common(g, p, bufs, scratch, scratch_bytes, nullptr, false, &b->launches);
     if (rc == FC_OK) *out = b.release();
     return rc;
+  });
+}
+
+int fc_operators_scratch_bytes(const fc_operator *ops, int32_t n, size_t *bytes) {
+  return guarded([&]() {
+    if (!bytes) return fail(FC_E_ARG, "null result pointer");
+    fc::OperatorList list;
+    std::string err;
+    const int rc = fc::check_operators(ops, n, list, err);
+    if (rc != FC_OK) return fail(rc, err);
+    *bytes = fc::operators_scratch_bytes(list);
+    return FC_OK;
+  });
+}
+
+int fc_run_operators(const fc_operator *ops, int32_t n, void *scratch, size_t scratch_bytes, void *hip_stream) {
+  return guarded([&]() {
+    fc::OperatorList list;
+    std::vector<fc::RecordedLaunch> launches;
+    std::string err;
+    int rc = fc::check_operators(ops, n, list, err);
+    if (rc == FC_OK) rc = fc::record_operators(list, scratch, scratch_bytes, launches, err);
+    if (rc == FC_OK) rc = fc::issue_recorded(launches, static_cast<hipStream_t>(hip_stream), err);
+    return rc == FC_OK ? rc : fail(rc, err);
+  });
+}
+
+int fc_bind_operators(const fc_operator *ops, int32_t n, void *scratch, size_t scratch_bytes, fc_bound **out) {
+  return guarded([&]() {
+    if (!out) return fail(FC_E_ARG, "null result pointer");
+    *out = nullptr;
+    auto b = std::make_unique<fc_bound>();
+    fc::OperatorList list;
+    std::string err;
+    int rc = fc::check_operators(ops, n, list, err);
+    if (rc == FC_OK) rc = fc::record_operators(list, scratch, scratch_bytes, b->launches, err);
+    if (rc != FC_OK) return fail(rc, err);
+    *out = b.release();
+    return FC_OK;
   });
 }
 

@@ -1,0 +1,518 @@
+// Norm of query and key heads with the rotation by position in the same pass, into tensors or into the cache, and its gradient
+// (include/fc.h, fc_head_norm_rope).
+//
+// One head of one token is a row of D elements.  2^log2 neighbouring lanes hold a row, each of them two packs of V elements
+// whose i-th elements are rotated together: (y[i], y[i + R/2]) lie R/2 apart, (y[2i], y[2i+1]) are the even and the odd elements of
+// two packs in a row; behind the rotated part the packs just follow each other.  So nothing is exchanged between lanes but the sum of
+// squares, and the row is read once and written once.  A wave takes one token after the other with some of its heads, so that
+// the token's cosines and sines and the weights are read once and stay in registers.
+#include "operators.hpp"
+
+#include <algorithm>
+
+namespace fc {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+
+struct Rows {                       // [T, heads, D]
+  char *ptr;
+  long long token, head;            // strides in elements
+};
+
+struct HeadsArgs {
+  Rows q, k, v, q_out, k_out;       // k_out: the tensor, or place 0 of the cache's pages (head: its stride)
+  char *v_cache;
+  const void *weight[2];            // of q and of k; NULL: no norm
+  const float *cos_sin;             // NULL: no rotation
+  const int *positions, *axis_of;
+  const long long *slots;           // NULL: keys go to the tensor
+  long long angle_stride, position_stride;
+  long long k_page, k_place, v_page, v_place, v_head;     // strides of the caches
+  unsigned tokens, heads[3];        // of q, k, v
+  unsigned dim, half, page, pages;  // half: R / 2
+  unsigned axes, angles;            // rows of positions and of cos_sin
+  unsigned lanes_log2, per_wave;    // lanes of a row; heads of a token that a wave takes
+  float eps;
+  bool wide_angles;                 // rows of cos_sin are aligned for packs
+};
+
+// by value: a choice between two places would put both into memory
+__device__ __forceinline__ float either(bool first, float a, float b) { return first ? a : b; }
+__device__ __forceinline__ Rows either(bool first, Rows a, Rows b) {
+  return {first ? a.ptr : b.ptr, first ? a.token : b.token, first ? a.head : b.head};
+}
+
+// Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.
+template <int V, bool Interleaved> struct Place {
+  unsigned at[2], pair;             // pair: of the first elements
+  bool any, turned;
+  __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
+    any = 2 * V * chunk < dim;
+    turned = V * chunk < half;
+    pair = V * chunk;
+    at[0] = turned && !Interleaved ? V * chunk : 2 * V * chunk;
+    at[1] = turned && !Interleaved ? half + V * chunk : 2 * V * chunk + V;
+  }
+};
+
+// zeros where there is nothing, or where `live` is false
+template <class T, int V, bool Interleaved>
+__device__ __forceinline__ void load_row(const T *row, const Place<V, Interleaved> &p, bool live, float (&x)[2][V]) {
+  Vec<T, V> a, b;
+#pragma unroll
+  for (int i = 0; i < V; ++i) a[i] = b[i] = (T)0.0f;
+  if (p.any && live) {
+    a = load_vec<T, V>(row + p.at[0]);
+    b = load_vec<T, V>(row + p.at[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if constexpr (Interleaved) {    // also behind the rotated part: the two packs follow each other there
+      const int e = 2 * i, o = 2 * i + 1;
+      x[0][i] = e < V ? (float)a[e % V] : (float)b[e % V];
+      x[1][i] = o < V ? (float)a[o % V] : (float)b[o % V];
+    } else {
+      x[0][i] = (float)a[i];
+      x[1][i] = (float)b[i];
+    }
+  }
+}
+
+template <class T, int V, bool Interleaved>
+__device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p, const float (&x)[2][V]) {
+  if (!p.any) return;
+  Vec<T, V> a, b;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if constexpr (Interleaved) {
+      const int e = 2 * i, o = 2 * i + 1;
+      if (e < V) a[e % V] = (T)x[0][i]; else b[e % V] = (T)x[0][i];
+      if (o < V) a[o % V] = (T)x[1][i]; else b[o % V] = (T)x[1][i];
+    } else {
+      a[i] = (T)x[0][i];
+      b[i] = (T)x[1][i];
+    }
+  }
+  store_vec<T, V>(row + p.at[0], a);
+  store_vec<T, V>(row + p.at[1], b);
+}
+
+// Cosines and sines of the pairs of this lane at token t: 1 and 0 where nothing is turned, NaN where the table has no row.
+template <int V, bool Interleaved>
+__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
+  const bool on = a.cos_sin && p.any && p.turned;
+  if (!a.axis_of) {                 // one position a token: the lane's pairs lie side by side
+    constexpr int N = V < 4 ? V : 4;
+    const int at = on && a.axes ? a.positions[t] : -1;
+    const bool there = (unsigned)at < a.angles;
+    const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + p.pair;
+#pragma unroll
+    for (int i = 0; i < V; i += N) {
+      const float missing = on ? __builtin_nanf("") : 1.0f;
+      Vec<float, N> cosine, sine;
+#pragma unroll
+      for (int k = 0; k < N; ++k) { cosine[k] = missing; sine[k] = missing - 1.0f; }
+      if (there) {
+        if (a.wide_angles) {
+          cosine = load_vec<float, N>(row + i);
+          sine = load_vec<float, N>(row + a.half + i);
+        } else {
+#pragma unroll
+          for (int k = 0; k < N; ++k) { cosine[k] = row[i + k]; sine[k] = row[a.half + i + k]; }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) { c[i + k] = cosine[k]; s[i + k] = sine[k]; }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float cosine = 1.0f, sine = 0.0f;
+    if (on) {
+      const int axis = a.axis_of[p.pair + i];
+      const int at = (unsigned)axis < a.axes ? a.positions[axis * a.position_stride + t] : -1;
+      const bool there = (unsigned)at < a.angles;
+      const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + p.pair + i;
+      cosine = there ? row[0] : __builtin_nanf("");
+      sine = there ? row[a.half] : __builtin_nanf("");
+    }
+    c[i] = cosine;
+    s[i] = sine;
+  }
+}
+
+template <class T, int V, bool Interleaved>
+__device__ __forceinline__ void load_weight(const HeadsArgs &a, int which, const Place<V, Interleaved> &p, float (&w)[2][V]) {
+  const bool any = a.weight[which] != nullptr;
+  load_row<T, V, Interleaved>(static_cast<const T *>(a.weight[which]), p, any, w);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    w[0][i] = any ? w[0][i] : 1.0f;
+    w[1][i] = any ? w[1][i] : 1.0f;
+  }
+}
+
+template <int V> __device__ __forceinline__ float sum_of_products(const float (&x)[2][V], const float (&y)[2][V]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) s = fmaf(x[1][i], y[1][i], fmaf(x[0][i], y[0][i], s));
+  return s;
+}
+
+// The units of work: a token with per_wave of its heads (q, k and v numbered in one row), a wave each.
+template <class T, int V, bool Interleaved>
+__global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
+  const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
+  const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
+  const Place<V, Interleaved> p(a.dim, a.half, chunk);
+  float wq[2][V], wk[2][V];
+  load_weight<T, V, Interleaved>(a, 0, p, wq);
+  load_weight<T, V, Interleaved>(a, 1, p, wk);
+  const unsigned heads = a.heads[0] + a.heads[1] + a.heads[2], parts = (heads + a.per_wave - 1) / a.per_wave;
+  const unsigned long long units = (unsigned long long)a.tokens * parts;
+  const float by_dim = 1.0f / (float)a.dim;
+  for (unsigned long long u = (unsigned long long)blockIdx.x * kWaves + wave_id(); u < units; u += (unsigned long long)gridDim.x * kWaves) {
+    const unsigned t = (unsigned)(u / parts), h0 = (unsigned)(u % parts) * a.per_wave;
+    float c[V], s[V];
+    load_angles(a, p, t, c, s);
+    const long long slot = a.slots ? a.slots[t] : 0;
+    const bool stored = !a.slots || (unsigned long long)slot < (unsigned long long)a.pages * a.page;
+    const unsigned page = a.slots && stored ? (unsigned)(slot / a.page) : 0u, place = a.slots && stored ? (unsigned)(slot - (long long)page * a.page) : 0u;
+    for (unsigned h = h0 + row_of_wave; h < min(h0 + a.per_wave, heads) + row_of_wave; h += rows) {   // the same number of turns for all lanes
+      const bool live = h < min(h0 + a.per_wave, heads);
+      const bool is_q = h < a.heads[0], is_v = h >= a.heads[0] + a.heads[1];
+      const unsigned head = is_q ? h : is_v ? h - a.heads[0] - a.heads[1] : h - a.heads[0];
+      const Rows from = either(is_q, a.q, either(is_v, a.v, a.k));
+      float x[2][V];
+      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(from.ptr) + t * from.token + head * from.head, p, live, x);
+      const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
+      if (!is_v) {
+        const float r = (is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? 1.0f / sqrtf(square * by_dim + a.eps) : 1.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float y0 = x[0][i] * r * either(is_q, wq[0][i], wk[0][i]), y1 = x[1][i] * r * either(is_q, wq[1][i], wk[1][i]);
+          x[0][i] = p.turned ? y0 * c[i] - y1 * s[i] : y0;
+          x[1][i] = p.turned ? y1 * c[i] + y0 * s[i] : y1;
+        }
+      }
+      if (!live || (!is_q && !stored)) continue;
+      T *to;
+      if (is_q) to = reinterpret_cast<T *>(a.q_out.ptr) + t * a.q_out.token + head * a.q_out.head;
+      else if (is_v) to = reinterpret_cast<T *>(a.v_cache) + page * a.v_page + place * a.v_place + head * a.v_head;
+      else if (a.slots) to = reinterpret_cast<T *>(a.k_out.ptr) + page * a.k_page + place * a.k_place + head * a.k_out.head;
+      else to = reinterpret_cast<T *>(a.k_out.ptr) + t * a.k_out.token + head * a.k_out.head;
+      store_row<T, V, Interleaved>(to, p, x);
+    }
+  }
+}
+
+constexpr unsigned kMostDim = 512;
+constexpr unsigned kGradGroups = 1024;      // workgroups of the gradient at most: one row of partial sums for each
+
+struct GradRows {
+  Rows dy[2], dx[2];                        // of q and of k
+};
+
+// dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
+
+template <class T, int V, bool Interleaved>
+__global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
+  __shared__ float sums[kWaves][2][kMostDim];
+  const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
+  const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
+  const Place<V, Interleaved> p(a.dim, a.half, chunk);
+  float wq[2][V], wk[2][V], dq[2][V], dk[2][V];
+  load_weight<T, V, Interleaved>(a, 0, p, wq);
+  load_weight<T, V, Interleaved>(a, 1, p, wk);
+#pragma unroll
+  for (int i = 0; i < V; ++i) dq[0][i] = dq[1][i] = dk[0][i] = dk[1][i] = 0.0f;
+  const unsigned heads = a.heads[0] + a.heads[1], parts = (heads + a.per_wave - 1) / a.per_wave;
+  const unsigned long long units = (unsigned long long)a.tokens * parts;
+  const float by_dim = 1.0f / (float)a.dim;
+  for (unsigned long long u = (unsigned long long)blockIdx.x * kWaves + wave_id(); u < units; u += (unsigned long long)gridDim.x * kWaves) {
+    const unsigned t = (unsigned)(u / parts), h0 = (unsigned)(u % parts) * a.per_wave;
+    float c[V], s[V];
+    load_angles(a, p, t, c, s);
+    for (unsigned h = h0 + row_of_wave; h < min(h0 + a.per_wave, heads) + row_of_wave; h += rows) {   // the same number of turns for all lanes
+      const bool live = h < min(h0 + a.per_wave, heads);
+      const bool is_q = h < a.heads[0];
+      const unsigned head = is_q ? h : h - a.heads[0];
+      const Rows from = either(is_q, a.q, a.k), up = either(is_q, rows_of.dy[0], rows_of.dy[1]);
+      float x[2][V], g[2][V];
+      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(from.ptr) + t * from.token + head * from.head, p, live, x);
+      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(up.ptr) + t * up.token + head * up.head, p, live, g);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float g0 = g[0][i], g1 = g[1][i];
+        if (p.turned) {
+          g[0][i] = g0 * c[i] + g1 * s[i];
+          g[1][i] = g1 * c[i] - g0 * s[i];
+        }
+      }
+      if (is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
+        // the sums are taken by all lanes of a row together: a row is of q or of k as a whole
+        const float r = 1.0f / sqrtf(lanes_sum(sum_of_products(x, x), (int)a.lanes_log2) * by_dim + a.eps);
+        float gw[2][V];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            x[k][i] *= r;
+            const float dw = live ? g[k][i] * x[k][i] : 0.0f;
+            dq[k][i] += is_q ? dw : 0.0f;
+            dk[k][i] += is_q ? 0.0f : dw;
+            gw[k][i] = g[k][i] * either(is_q, wq[k][i], wk[k][i]);
+          }
+        const float mean = lanes_sum(sum_of_products(gw, x), (int)a.lanes_log2) * by_dim;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) g[k][i] = r * (gw[k][i] - x[k][i] * mean);
+      }
+      if (!live) continue;
+      const Rows to = either(is_q, rows_of.dx[0], rows_of.dx[1]);
+      store_row<T, V, Interleaved>(reinterpret_cast<T *>(to.ptr) + t * to.token + head * to.head, p, g);
+    }
+  }
+  if (!partial) return;
+  // over the rows of the wave, then over the waves
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      for (unsigned d = lanes; d < (unsigned)kWave; d *= 2) {
+        dq[k][i] += __shfl_xor(dq[k][i], (int)d);
+        dk[k][i] += __shfl_xor(dk[k][i], (int)d);
+      }
+  if (row_of_wave == 0) {
+    store_row<float, V, Interleaved>(sums[wave_id()][0], p, dq);
+    store_row<float, V, Interleaved>(sums[wave_id()][1], p, dk);
+  }
+  __syncthreads();
+  for (unsigned i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
+    const unsigned which = i >= a.dim, d = i - which * a.dim;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w][which][d];
+    partial[(unsigned long long)blockIdx.x * 2 * a.dim + i] = sum;
+  }
+}
+
+// dw[i] = sum of partial[g][i] over the groups: 16 columns a workgroup, 16 threads a column
+__global__ __launch_bounds__(kThreads) void weight_grad_kernel(const float *partial, unsigned groups, unsigned dim, float *dq, float *dk) {
+  __shared__ float sums[16][17];
+  const unsigned column = blockIdx.x * 16 + (threadIdx.x & 15), of = threadIdx.x >> 4;
+  float sum = 0.0f;
+  if (column < 2 * dim)
+    for (unsigned g = of; g < groups; g += 16) sum += partial[(unsigned long long)g * 2 * dim + column];
+  sums[of][threadIdx.x & 15] = sum;
+  __syncthreads();
+  if (of != 0 || column >= 2 * dim) return;
+  sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) sum += sums[k][threadIdx.x];
+  float *to = column < dim ? dq : dk;
+  if (to) to[column < dim ? column : column - dim] = sum;
+}
+
+// ------------------------------------------------------------------ host
+// calls f with the type, the elements of a pack and the pairing of this call as compile-time values
+template <class F> void with_form(int32_t dtype, int pack, bool interleaved, F &&f) {
+  auto by_pack = [&](auto element, auto paired) {
+    using T = decltype(element);
+    if constexpr (sizeof(T) == 2)
+      if (pack == 8) { f(element, std::integral_constant<int, 8>{}, paired); return; }
+    if (pack == 4) f(element, std::integral_constant<int, 4>{}, paired);
+    else if (pack == 2) f(element, std::integral_constant<int, 2>{}, paired);
+    else f(element, std::integral_constant<int, 1>{}, paired);
+  };
+  auto by_pairing = [&](auto element) { interleaved ? by_pack(element, std::true_type{}) : by_pack(element, std::false_type{}); };
+  if (dtype == FC_F32) by_pairing(float{});
+  else if (dtype == FC_F16) by_pairing(_Float16{});
+  else by_pairing(__bf16{});
+}
+
+Rows rows_at(const fc_tensor &t) { return {static_cast<char *>(t.ptr), t.stride[0], t.stride[1]}; }
+
+struct HeadsCall {
+  HeadsArgs a{};
+  int32_t dtype;
+  int pack;
+  bool interleaved;
+  // how the heads of a token are shared among waves, and the workgroups that are then needed, `most` at most
+  unsigned shape(unsigned heads, unsigned most) {
+    const unsigned rows = kWave >> a.lanes_log2;
+    // a wave takes all heads of a token, unless that leaves compute units without work
+    const unsigned turns = ceil_div(heads, rows);
+    const unsigned parts = std::min<unsigned>(turns, std::max(1u, 4096u / std::max(1u, a.tokens)));
+    a.per_wave = ceil_div(turns, parts) * rows;
+    return std::min(std::max(ceil_div((unsigned long long)a.tokens * ceil_div(heads, a.per_wave), kWaves), 1u), most);
+  }
+};
+
+// what the operator and its gradient have in common
+int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const fc_tensor &q_weight, const fc_tensor &k_weight, const fc_tensor &cos_sin,
+                const fc_tensor &positions, const fc_tensor &axis_of, double eps, int32_t interleaved, HeadsCall &call) {
+  const int32_t dtype = q.dtype;
+  if (dtype != FC_F32 && dtype != FC_F16 && dtype != FC_BF16) return c.fail(FC_E_ARG, "q: type f32, f16 or bf16 is needed").code();
+  c.array("q", q, dtype, {-1, -1, -1});
+  if (!c.ok()) return c.code();
+  const int64_t tokens = q.shape[0], dim = q.shape[2];
+  c.array("k", k, dtype, {tokens, -1, dim});
+  if (present(q_weight)) c.array("q_weight", q_weight, dtype, {dim});
+  if (present(k_weight)) c.array("k_weight", k_weight, dtype, {dim});
+  if (present(cos_sin)) {
+    c.array("cos_sin", cos_sin, FC_F32, {-1, -1});
+    c.array("positions", positions, FC_I32, {-1, tokens});
+    if (c.ok() && (cos_sin.shape[1] % 2 || cos_sin.shape[1] > dim)) c.fail(FC_E_ARG, "cos_sin: an even number of columns, at most the elements of a head, is needed");
+    if (present(axis_of)) c.array("axis_of", axis_of, FC_I32, {cos_sin.shape[1] / 2});
+  } else if (present(positions) || present(axis_of)) {
+    c.fail(FC_E_ARG, "positions and axis_of go with cos_sin");
+  }
+  if (c.ok() && !(eps >= 0)) c.fail(FC_E_ARG, "eps must not be negative");
+  if (c.ok() && (dim < 2 || dim % 2 || dim > (int64_t)kMostDim)) c.fail(FC_E_UNSUPPORTED, "heads have an even number of elements, at most 512");
+  if (c.ok() && tokens * (q.shape[1] + k.shape[1]) > (int64_t)1 << 40) c.fail(FC_E_LIMIT, "too many heads");
+  if (!c.ok()) return c.code();
+  HeadsArgs &a = call.a;
+  a.q = rows_at(q);
+  a.k = rows_at(k);
+  a.weight[0] = present(q_weight) ? q_weight.ptr : nullptr;
+  a.weight[1] = present(k_weight) ? k_weight.ptr : nullptr;
+  if (present(cos_sin) && cos_sin.shape[1] > 0) {
+    a.half = (unsigned)cos_sin.shape[1] / 2;
+    a.cos_sin = static_cast<const float *>(cos_sin.ptr);
+    a.positions = static_cast<const int *>(positions.ptr);
+    a.axis_of = present(axis_of) ? static_cast<const int *>(axis_of.ptr) : nullptr;
+    a.angle_stride = cos_sin.stride[0];
+    a.position_stride = positions.stride[0];
+    a.angles = (unsigned)cos_sin.shape[0];
+    a.axes = (unsigned)positions.shape[0];
+  }
+  a.tokens = (unsigned)tokens;
+  a.heads[0] = (unsigned)q.shape[1];
+  a.heads[1] = (unsigned)k.shape[1];
+  a.dim = (unsigned)dim;
+  a.eps = (float)eps;
+  call.dtype = dtype;
+  call.interleaved = interleaved != 0;
+  // 16 bytes a pack, less where the pairs, the strides or the alignment of an array do not allow it
+  call.pack = 16 / size_of_dtype(dtype);
+  while (call.pack > 1 && (a.half % call.pack || dim / 2 % call.pack)) call.pack /= 2;
+  a.wide_angles = a.cos_sin && common_alignment(cos_sin, 4) == 4;
+  for (const fc_tensor *t : {&q, &k, &q_weight, &k_weight})
+    if (present(*t)) call.pack = common_alignment(*t, call.pack);
+  return FC_OK;
+}
+
+// once the packs are known
+int settle_lanes(TensorChecks &c, HeadsCall &call) {
+  unsigned lanes = 1;
+  while (lanes * 2 * call.pack < call.a.dim) { lanes *= 2; ++call.a.lanes_log2; }
+  if (lanes > (unsigned)kWave)
+    return c.fail(FC_E_UNSUPPORTED, "heads of " + std::to_string(call.a.dim) + " elements can be read " + std::to_string(call.pack) +
+                                        " at a time only (rotated pairs, strides and alignment): at most " + std::to_string(128 * call.pack) + " are built for").code();
+  return FC_OK;
+}
+
+struct HeadNormRope final : Operator, HeadsCall {
+  unsigned grid = 0;
+  void record(Recorder &r) const override {
+    if (a.tokens == 0 || a.heads[0] + a.heads[1] + a.heads[2] == 0) return;
+    with_form(dtype, pack, interleaved, [&](auto element, auto v, auto paired) {
+      r.launch(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value>, grid, kThreads, a);
+    });
+  }
+  const char *name() const override { return "head norm and rotation"; }
+};
+
+struct HeadNormRopeGrad final : Operator, HeadsCall {
+  GradRows rows{};
+  float *dw[2] = {nullptr, nullptr};
+  unsigned grid = 0;
+  size_t workspace() const override { return dw[0] || dw[1] ? (size_t)grid * 2 * a.dim * sizeof(float) : 0; }
+  void record(Recorder &r) const override {
+    float *partial = dw[0] || dw[1] ? reinterpret_cast<float *>(r.workspace) : nullptr;
+    if (!partial && (a.tokens == 0 || a.heads[0] + a.heads[1] == 0)) return;
+    with_form(dtype, pack, interleaved, [&](auto element, auto v, auto paired) {
+      r.launch(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value>, grid, kThreads, a, rows, partial);
+    });
+    if (partial) r.launch(&weight_grad_kernel, ceil_div(2 * a.dim, 16), kThreads, (const float *)partial, grid, a.dim, dw[0], dw[1]);
+  }
+  const char *name() const override { return "gradient of head norm and rotation"; }
+};
+
+}  // namespace
+
+int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &out, std::string &err) {
+  TensorChecks c(err);
+  auto op = std::make_unique<HeadNormRope>();
+  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, *op) != FC_OK) return c.code();
+  HeadsArgs &a = op->a;
+  const int64_t tokens = a.tokens, dim = a.dim, kv = a.heads[1];
+  c.array("q_out", n.q_out, op->dtype, {tokens, a.heads[0], dim}, true);
+  a.q_out = rows_at(n.q_out);
+  auto align = [&](const fc_tensor &t) { op->pack = common_alignment(t, op->pack); };
+  if (present(n.slots)) {
+    if (present(n.k_out)) c.fail(FC_E_ARG, "keys go to k_out or, with slots, to the cache");
+    c.array("slots", n.slots, FC_I64, {tokens});
+    c.array("v", n.v, op->dtype, {tokens, kv, dim});
+    c.array("k_cache", n.k_cache, op->dtype, {-1, -1, kv, dim}, true);
+    c.array("v_cache", n.v_cache, op->dtype, {n.k_cache.shape[0], n.k_cache.shape[1], kv, dim}, true);
+    if (c.ok() && n.k_cache.shape[1] < 1) c.fail(FC_E_ARG, "k_cache: pages without places");
+    if (!c.ok()) return c.code();
+    a.slots = static_cast<const long long *>(n.slots.ptr);
+    a.heads[2] = (unsigned)kv;
+    a.v = rows_at(n.v);
+    a.pages = (unsigned)n.k_cache.shape[0];
+    a.page = (unsigned)n.k_cache.shape[1];
+    a.k_out = {static_cast<char *>(n.k_cache.ptr), 0, n.k_cache.stride[2]};
+    a.v_cache = static_cast<char *>(n.v_cache.ptr);
+    a.k_page = n.k_cache.stride[0];
+    a.k_place = n.k_cache.stride[1];
+    a.v_page = n.v_cache.stride[0];
+    a.v_place = n.v_cache.stride[1];
+    a.v_head = n.v_cache.stride[2];
+    for (const fc_tensor *t : {&n.v, &n.k_cache, &n.v_cache}) align(*t);
+  } else {
+    if (present(n.v) || present(n.k_cache) || present(n.v_cache)) c.fail(FC_E_ARG, "v and the caches go with slots");
+    c.array("k_out", n.k_out, op->dtype, {tokens, kv, dim}, true);
+    a.k_out = rows_at(n.k_out);
+    align(n.k_out);
+  }
+  if (!c.ok()) return c.code();
+  align(n.q_out);
+  if (settle_lanes(c, *op) != FC_OK) return c.code();
+  op->grid = op->shape(a.heads[0] + a.heads[1] + a.heads[2], 4096);
+  out = std::move(op);
+  return FC_OK;
+}
+
+int make_head_norm_rope_grad(const fc_head_norm_rope_grad &n, std::unique_ptr<Operator> &out, std::string &err) {
+  TensorChecks c(err);
+  auto op = std::make_unique<HeadNormRopeGrad>();
+  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, *op) != FC_OK) return c.code();
+  HeadsArgs &a = op->a;
+  const int64_t tokens = a.tokens, dim = a.dim;
+  c.array("dq_out", n.dq_out, op->dtype, {tokens, a.heads[0], dim});
+  c.array("dk_out", n.dk_out, op->dtype, {tokens, a.heads[1], dim});
+  c.array("dq", n.dq, op->dtype, {tokens, a.heads[0], dim}, true);
+  c.array("dk", n.dk, op->dtype, {tokens, a.heads[1], dim}, true);
+  if (present(n.q_weight) != present(n.dq_weight) || present(n.k_weight) != present(n.dk_weight))
+    c.fail(FC_E_ARG, "a weight and its gradient are there together or not at all");
+  if (present(n.dq_weight)) c.array("dq_weight", n.dq_weight, FC_F32, {dim}, true);
+  if (present(n.dk_weight)) c.array("dk_weight", n.dk_weight, FC_F32, {dim}, true);
+  if (!c.ok()) return c.code();
+  op->rows = {{rows_at(n.dq_out), rows_at(n.dk_out)}, {rows_at(n.dq), rows_at(n.dk)}};
+  for (const fc_tensor *t : {&n.dq_out, &n.dk_out, &n.dq, &n.dk}) op->pack = common_alignment(*t, op->pack);
+  if (settle_lanes(c, *op) != FC_OK) return c.code();
+  op->dw[0] = present(n.dq_weight) ? static_cast<float *>(n.dq_weight.ptr) : nullptr;
+  op->dw[1] = present(n.dk_weight) ? static_cast<float *>(n.dk_weight.ptr) : nullptr;
+  op->grid = op->shape(a.heads[0] + a.heads[1], kGradGroups);
+  out = std::move(op);
+  return FC_OK;
+}
+
+}  // namespace fc
