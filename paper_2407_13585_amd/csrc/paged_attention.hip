@@ -2,7 +2,20 @@
 //
 // A gather through the block table fused into a fold whose state is (running maximum m, running sum l, weighted sum o):
 // a key with score s turns it into (m', l e^(m-m') + e^(s-m'), o e^(m-m') + e^(s-m') v), m' = max(m, s), and two states join the
-// same way.  A workgroup takes one query head of one request; its waves take 64 keys in turn and join at the end.
+// same way.
+//
+// The query heads of a group read the same keys: 16 of them are the columns of the matrix instructions, so a key is read once
+// for all of them.  A wave takes 32 keys (16 of 32 bits) at a time and exchanges nothing with other waves until its keys are done:
+//   scores  = K q^T     rows: keys,     columns: heads, sum over d;  lane (r, g), r = lane % 16, g = lane / 16, gets those of head r and
+//                       the keys 4g .. 4g+3 of every 16
+//   outputs = V^T p^T   rows: d,        columns: heads, sum over keys
+// The sum over keys takes them in any order, so a lane passes the weights on where the scores left them, and reads the values of
+// just these keys, d = W r .. W r + W-1 (W = D / 16) of each: rows of V are read whole and in order, and the transposition is
+// a permutation of a lane's own registers.
+//
+// The keys of all requests and key heads are one long row of units of 128 (64) keys, of which every workgroup takes an equal share,
+// whatever the lengths are: what is long is split, what is short is taken together.  Pieces of a split row go to scratch and
+// are joined in their order by a second kernel.
 #include "operators.hpp"
 
 #include <cmath>
@@ -13,96 +26,402 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr unsigned kMostDim = 256;
+constexpr int kColumns = 16;               // query heads of a group that are taken together
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 struct AttentionArgs {
   const char *q, *k, *v;
   const int *table, *lengths;
   char *out;
-  float *lse;                       // NULL: not wanted
+  float *lse;                              // NULL: not wanted
+  float *pieces;                           // DEVICE: two pieces a workgroup
   long long q_request, q_head, out_request, out_head, lse_request, table_stride;
   long long k_page, k_place, k_head, v_page, v_place, v_head;
-  unsigned heads, group, dim, page, pages, width, window;
-  float scale;
+  unsigned requests, kv_heads, group, tiles, dim, page, pages, width, window;      // tiles: a group's heads, 16 at a time
+  unsigned workers, least_share;
+  float scale;                             // times log2(e)
 };
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
-  __shared__ float query[kMostDim], weights[kWaves][kWave], sums[kWaves][kMostDim], tops[kWaves], totals[kWaves];
-  const unsigned b = blockIdx.y, h = blockIdx.x, kv = h / a.group;
-  const T *q = reinterpret_cast<const T *>(a.q) + b * a.q_request + h * a.q_head;
-  for (unsigned d = threadIdx.x; d < a.dim; d += kThreads) query[d] = (float)q[d] * a.scale;
-  __syncthreads();
-  const int length = max(a.lengths[b], 0);
-  const unsigned begin = a.window && (unsigned)length > a.window ? (unsigned)length - a.window : 0u;
-  const unsigned end = (unsigned)min((unsigned long long)length, (unsigned long long)a.width * a.page);
-  const int *table = a.table + b * a.table_stride;
-  float top = -__builtin_inff(), total = 0.0f, o[kMostDim / kWave] = {};
-  for (unsigned j0 = begin + wave_id() * kWave; j0 < end; j0 += kThreads) {
-    const unsigned j = j0 + lane_id();
-    const unsigned page = j < end ? (unsigned)table[j / a.page] : a.pages;
-    float s = -__builtin_inff();
-    if (page < a.pages) {
-      const T *k = reinterpret_cast<const T *>(a.k) + page * a.k_page + j % a.page * a.k_place + kv * a.k_head;
-      s = 0.0f;
-      for (unsigned d = 0; d < a.dim; d += 8) {
-        const Vec<T, 8> x = load_vec<T, 8>(k + d);
+// What the types differ in.  kKeys: keys of a wave's step; kShift: the weights are held 2^kShift larger, which keeps the small ones
+// of 16-bit floats off their smallest numbers.
+template <class T> struct Kind { static constexpr int kKeys = 32, kShift = 0; };
+template <> struct Kind<_Float16> { static constexpr int kKeys = 32, kShift = 14; };
+template <> struct Kind<float> { static constexpr int kKeys = 16, kShift = 0; };
+
+template <class T> constexpr int kUnit = Kind<T>::kKeys * kWaves;
+
+using Acc = Vec<float, 4>;
+__device__ __forceinline__ Acc mma(Vec<__bf16, 8> a, Vec<__bf16, 8> b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ Acc mma(Vec<_Float16, 8> a, Vec<_Float16, 8> b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ Acc mma(Vec<float, 4> a, Vec<float, 4> b, Acc c) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(query[d + i], (float)x[i], s);
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+// A weight as two numbers of 16 bits: the upper part cut off, not rounded, so that the rest is not negative, and the rest never 0, so
+// that an infinite value times a weight stays that infinity in both products.  Together 16 bits (bf16) or 22 of the weight.
+__device__ __forceinline__ void split(float p, __bf16 &high, __bf16 &low) {
+  const float cut = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+  high = (__bf16)cut;
+  low = (__bf16)fmaxf(p - cut, 0x1p-126f);
+}
+__device__ __forceinline__ void split(float p, _Float16 &high, _Float16 &low) {
+  high = (_Float16)__builtin_amdgcn_cvt_pkrtz(p, 0.0f)[0];
+  low = (_Float16)fmaxf(p - (float)high, 0x1p-24f);
+}
+
+// over the lanes of a head: lane, lane ^ 16, lane ^ 32, lane ^ 48
+__device__ __forceinline__ float column_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// Keys of a request: [begin, end), from the step boundary `from` on in `units` units.
+struct Span {
+  unsigned begin, end, from, units;
+};
+template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &a, unsigned b) {
+  const int length = a.lengths[b];
+  Span s;
+  s.end = (unsigned)min((unsigned long long)max(length, 0), (unsigned long long)a.width * a.page);
+  s.begin = a.window && length > 0 && (unsigned)length > a.window ? (unsigned)length - a.window : 0u;
+  s.from = s.begin / Kind<T>::kKeys * Kind<T>::kKeys;
+  s.units = s.end > s.begin ? (s.end - s.from + kUnit<T> - 1) / kUnit<T> : 0u;
+  return s;
+}
+
+// This workgroup's share of all units: units [at, end) of the row, the first of them `offset` units into request `request`.
+struct Share {
+  unsigned long long at, end, offset, share;
+  unsigned request;
+};
+
+template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs &a, unsigned worker) {
+  __shared__ unsigned long long sums[kWaves], found_offset;
+  __shared__ unsigned found;
+  const unsigned rows = a.kv_heads * a.tiles, each = (a.requests + kThreads - 1) / kThreads;
+  const unsigned b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
+  unsigned long long mine = 0;
+  for (unsigned b = b0; b < b1; ++b) mine += span_of<T>(a, b).units;
+  mine *= rows;
+  unsigned long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const unsigned long long u = __shfl_up(upto, d);
+    if (lane_id() >= d) upto += u;
+  }
+  if (lane_id() == kWave - 1) sums[wave_id()] = upto;
+  __syncthreads();
+  unsigned long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave_id()) before += sums[w];
+    total += sums[w];
+  }
+  Share s;
+  s.share = max((total + a.workers - 1) / a.workers, (unsigned long long)a.least_share);
+  s.at = min(worker * s.share, total);
+  s.end = min(s.at + s.share, total);
+  before += upto - mine;
+  if (s.at >= before && s.at < before + mine) {
+    unsigned b = b0;
+    for (;; ++b) {
+      const unsigned long long here = (unsigned long long)span_of<T>(a, b).units * rows;
+      if (s.at < before + here) break;
+      before += here;
+    }
+    found = b;
+    found_offset = s.at - before;
+  }
+  __syncthreads();
+  s.request = s.at < s.end ? found : 0u;
+  s.offset = s.at < s.end ? found_offset : 0ull;
+  return s;
+}
+
+// floats of a piece: the weighted sums of the heads, then (m, l) of each
+__device__ __host__ __forceinline__ unsigned rows_of_piece(unsigned group) { return group < (unsigned)kColumns ? group : (unsigned)kColumns; }
+__device__ __host__ __forceinline__ unsigned long long piece_floats(unsigned group, unsigned dim) { return (unsigned long long)rows_of_piece(group) * (dim + 2); }
+
+template <class T, int Dim, bool Plain> struct Wave {
+  static constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = 16 / sizeof(T);      // kWide: elements of 16 bytes
+  static constexpr int kChunks = Dim / (4 * kWide);          // of K: 16 bytes of each of 4 lanes
+  static constexpr int kW = Dim / 16;                        // d of a lane in V
+  static constexpr int kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;  // ... in loads of 16 bytes at most
+  using Frag = Vec<T, kWide>;
+  using Part = Vec<T, kPart>;
+
+  Frag q[kChunks];
+  Acc o[kW];
+  float m, l;
+
+  __device__ __forceinline__ void start(const AttentionArgs &a, const T *heads, unsigned count) {
+    const unsigned r = lane_id() & 15, g = lane_id() >> 4;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const unsigned d = (c * 4 + g) * kWide;
+#pragma unroll
+      for (int i = 0; i < kWide; ++i) q[c][i] = r < count && d + i < a.dim ? heads[r * a.q_head + d + i] : (T)0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kW; ++j) o[j] = Acc{0.0f, 0.0f, 0.0f, 0.0f};
+    m = -__builtin_inff();
+    l = 0.0f;
+  }
+
+  // the keys j0 .. j0 + kKeys - 1, j0 a multiple of kKeys
+  __device__ __forceinline__ void step(const AttentionArgs &a, const Span &s, const int *table, const T *k, const T *v, unsigned j0) {
+    const unsigned r = lane_id() & 15, g = lane_id() >> 4;
+    Frag kf[kSub][kChunks];
+    Part vf[kSub][4][kParts];
+    bool there[kSub][4];                                     // the keys whose scores this lane gets
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) {
+      const unsigned j = j0 + 16 * u + r;
+      unsigned page = a.pages, place = 0;
+      if (j >= s.begin && j < s.end) {
+        const unsigned at = j / a.page;
+        page = (unsigned)table[at];
+        place = j - at * a.page;
+      }
+      const bool mine = page < a.pages;
+      const T *row = k + (mine ? page * a.k_page + place * a.k_place : 0ll);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const unsigned d = (c * 4 + g) * kWide;
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
+        if (mine && (Plain || d < a.dim)) f = load_vec<T, kWide>(row + d);
+        kf[u][c] = f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned vp = __shfl(page, (int)(4 * g + i)), vo = __shfl(place, (int)(4 * g + i));
+        there[u][i] = vp < a.pages;
+        const T *values = v + (there[u][i] ? vp * a.v_page + vo * a.v_place : 0ll) + r * kW;
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) {
+          Part f;
+#pragma unroll
+          for (int e = 0; e < kPart; ++e) f[e] = (T)0.0f;
+          if (there[u][i]) {
+            // heads have a multiple of 8 elements, a part 4 or 8: it is there as a whole or not at all
+            if (Plain || r * kW + n * kPart < a.dim) f = load_vec<T, kPart>(values + n * kPart);
+          }
+          vf[u][i][n] = f;
+        }
       }
     }
-    float most = s;
+    float p[kSub][4], most = -__builtin_inff();
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    most = fmaxf(most, top);
-    const float base = most == -__builtin_inff() ? 0.0f : most;
-    const float p = page < a.pages ? expf(s - base) : 0.0f, keep = expf(top - base);
-    float sum = p;
+    for (int u = 0; u < kSub; ++u) {
+      Acc score = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
-    total = total * keep + sum;
-    top = most;
-    weights[wave_id()][lane_id()] = p;
-    __builtin_amdgcn_wave_barrier();
+      for (int c = 0; c < kChunks; ++c) score = mma(kf[u][c], q[c], score);
 #pragma unroll
-    for (int i = 0; i < (int)(kMostDim / kWave); ++i) o[i] *= keep;
-    for (unsigned n = 0; n < (unsigned)kWave; ++n) {
-      const unsigned at = __shfl(page, (int)n), jn = j0 + n;
-      if (at >= a.pages) continue;
-      const float weight = weights[wave_id()][n];
-      const T *v = reinterpret_cast<const T *>(a.v) + at * a.v_page + jn % a.page * a.v_place + kv * a.v_head;
-#pragma unroll
-      for (int i = 0; i < (int)(kMostDim / kWave); ++i)
-        if (i * kWave + lane_id() < (int)a.dim) o[i] = fmaf(weight, (float)v[i * kWave + lane_id()], o[i]);
+      for (int i = 0; i < 4; ++i) {
+        p[u][i] = there[u][i] ? score[i] * a.scale : -__builtin_inff();
+        most = fmaxf(most, p[u][i]);
+      }
     }
-    __builtin_amdgcn_wave_barrier();
-  }
-  if (lane_id() == 0) { tops[wave_id()] = top; totals[wave_id()] = total; }
+    most = fmaxf(column_max(most), m);
+    const float top = most == -__builtin_inff() ? 0.0f : most, base = top - (float)Kind<T>::kShift;
+    const float keep = __builtin_amdgcn_exp2f(m - top);
+    m = most;
+    l *= keep;
 #pragma unroll
-  for (int i = 0; i < (int)(kMostDim / kWave); ++i) sums[wave_id()][i * kWave + lane_id()] = o[i];
-  __syncthreads();
-  float most = tops[0];
-  for (int w = 1; w < kWaves; ++w) most = fmaxf(most, tops[w]);
-  const float base = most == -__builtin_inff() ? 0.0f : most;
-  float l = 0.0f;
-  for (int w = 0; w < kWaves; ++w) l += totals[w] * expf(tops[w] - base);
-  for (unsigned d = threadIdx.x; d < a.dim; d += kThreads) {
-    float x = 0.0f;
-    for (int w = 0; w < kWaves; ++w) x += sums[w][d] * expf(tops[w] - base);
-    reinterpret_cast<T *>(a.out)[b * a.out_request + h * a.out_head + d] = (T)(l == 0.0f ? 0.0f : x / l);
+    for (int u = 0; u < kSub; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[u][i] = __builtin_amdgcn_exp2f(p[u][i] - base);
+        l += p[u][i];
+      }
+#pragma unroll
+    for (int j = 0; j < kW; ++j) o[j] *= keep;
+    if constexpr (sizeof(T) == 2) {
+      Vec<T, 8> high, low;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        T upper, rest;
+        split(p[e / 4][e % 4], upper, rest);
+        high[e] = upper;
+        low[e] = rest;
+      }
+#pragma unroll
+      for (int j = 0; j < kW; ++j) {
+        Vec<T, 8> values;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) values[e] = vf[e / 4][e % 4][j / kPart][j % kPart];
+        o[j] = mma(values, high, o[j]);
+        o[j] = mma(values, low, o[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kW; ++j)
+        o[j] = mma(Vec<float, 4>{vf[0][0][j / kPart][j % kPart], vf[0][1][j / kPart][j % kPart], vf[0][2][j / kPart][j % kPart], vf[0][3][j / kPart][j % kPart]},
+                   Vec<float, 4>{p[0][0], p[0][1], p[0][2], p[0][3]}, o[j]);
+    }
   }
-  if (a.lse && threadIdx.x == 0) a.lse[b * a.lse_request + h] = l == 0.0f ? -__builtin_inff() : base + logf(l);
+};
+
+template <class T> __device__ __forceinline__ void write_result(const AttentionArgs &a, unsigned b, unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) {
+  Vec<T, 4> x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = (T)(l == 0.0f ? 0.0f : sum[i] / l);
+  T *to = reinterpret_cast<T *>(a.out) + b * a.out_request + head * a.out_head + d;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to[i] = x[i];
+  if (a.lse && d == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : (m - (float)Kind<T>::kShift + __log2f(l)) * kLn2;
+}
+
+template <class T, int Dim, bool Plain>
+__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
+  __shared__ float sums[kWaves][kColumns][Dim + 4];          // + 4: the heads' rows start at different banks
+  __shared__ float tops[kWaves][kColumns], totals[kWaves][kColumns];
+  const unsigned rows = a.kv_heads * a.tiles, worker = blockIdx.x;
+  const unsigned r = lane_id() & 15, g = lane_id() >> 4;
+  for (unsigned b = worker; b < a.requests; b += a.workers) {          // requests without a key
+    if (span_of<T>(a, b).units) continue;
+    for (unsigned i = threadIdx.x; i < a.kv_heads * a.group * (a.dim / 4); i += kThreads)
+      write_result<T>(a, b, i / (a.dim / 4), i % (a.dim / 4) * 4, Vec<float, 4>{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f, 0.0f);
+  }
+  Share s = share_of<T>(a, worker);
+  bool first = true;
+  while (s.at < s.end) {
+    const unsigned b = __builtin_amdgcn_readfirstlane(s.request);
+    const Span span = span_of<T>(a, b);
+    if (s.offset >= (unsigned long long)span.units * rows) { s.offset -= (unsigned long long)span.units * rows; ++s.request; continue; }
+    const unsigned row = __builtin_amdgcn_readfirstlane((unsigned)(s.offset / span.units)), unit0 = (unsigned)(s.offset - (unsigned long long)row * span.units);
+    const unsigned unit1 = (unsigned)min((unsigned long long)span.units, unit0 + (s.end - s.at));
+    const unsigned kv = row / a.tiles, head0 = kv * a.group + row % a.tiles * kColumns;
+    const unsigned count = min((unsigned)kColumns, (kv + 1) * a.group - head0);
+    Wave<T, Dim, Plain> w;
+    w.start(a, reinterpret_cast<const T *>(a.q) + b * a.q_request + head0 * a.q_head, count);
+    const int *table = a.table + b * a.table_stride;
+    const T *k = reinterpret_cast<const T *>(a.k) + kv * a.k_head, *v = reinterpret_cast<const T *>(a.v) + kv * a.v_head;
+    for (unsigned unit = unit0; unit < unit1; ++unit) {
+      const unsigned j0 = span.from + unit * kUnit<T> + wave_id() * Kind<T>::kKeys;
+      if (j0 < span.end) w.step(a, span, table, k, v, j0);
+    }
+    const float total = column_sum(w.l);
+    __syncthreads();                                         // the row before is read
+    if (g == 0) { tops[wave_id()][r] = w.m; totals[wave_id()][r] = total; }
+    if (r < count)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < Dim / 16; j += 4) {
+          Vec<float, 4> x = {w.o[j][i], w.o[j + 1][i], w.o[j + 2][i], w.o[j + 3][i]};
+          *reinterpret_cast<Vec<float, 4> *>(&sums[wave_id()][r][(4 * g + i) * (Dim / 16) + j]) = x;
+        }
+    __syncthreads();
+    const bool whole = unit0 == 0 && unit1 == span.units;
+    float *piece = a.pieces + (worker * 2ull + !first) * piece_floats(a.group, a.dim);
+    for (unsigned i = threadIdx.x; i < count * (Dim / 4); i += kThreads) {
+      const unsigned head = i / (Dim / 4), d = i % (Dim / 4) * 4;
+      if (d >= a.dim) continue;
+      float most = tops[0][head], sum_l = 0.0f;
+#pragma unroll
+      for (int n = 1; n < kWaves; ++n) most = fmaxf(most, tops[n][head]);
+      Vec<float, 4> x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < kWaves; ++n) {
+        const float f = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(tops[n][head] - most);
+        sum_l += totals[n][head] * f;
+        x += *reinterpret_cast<const Vec<float, 4> *>(&sums[n][head][d]) * f;
+      }
+      if (whole) write_result<T>(a, b, head0 + head, d, x, most, sum_l);
+      else {
+        *reinterpret_cast<Vec<float, 4> *>(piece + head * a.dim + d) = x;
+        if (d == 0) {
+          piece[rows_of_piece(a.group) * a.dim + 2 * head] = most;
+          piece[rows_of_piece(a.group) * a.dim + 2 * head + 1] = sum_l;
+        }
+      }
+    }
+    first = false;
+    s.at += unit1 - unit0;
+    s.offset += unit1 - unit0;
+  }
+}
+
+// The pieces of a row that the worker before left unfinished and this one ended, for head blockIdx.y of its columns.
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs a) {
+  __shared__ float tops[kWaves], totals[kWaves], sums[kWaves][kMostDim];
+  const unsigned worker = blockIdx.x;
+  const Share s = share_of<T>(a, worker);
+  if (s.at >= s.end) return;
+  const Span span = span_of<T>(a, s.request);
+  const unsigned row = (unsigned)(s.offset / span.units), unit0 = (unsigned)(s.offset - (unsigned long long)row * span.units);
+  if (unit0 == 0 || span.units - unit0 > s.end - s.at) return;         // nothing is left over from before, or it goes on
+  const unsigned kv = row / a.tiles, head = kv * a.group + row % a.tiles * kColumns + blockIdx.y;
+  if (head >= (kv + 1) * a.group) return;
+  const unsigned long long start = s.at - unit0;                       // of the row
+  const unsigned w0 = (unsigned)(start / s.share);
+  const unsigned long long size = piece_floats(a.group, a.dim), ends = (unsigned long long)rows_of_piece(a.group) * a.dim + 2 * blockIdx.y;
+  // the first piece is its worker's last, the others are their workers' first
+  auto piece = [&](unsigned w) { return a.pieces + (w * 2ull + (w == w0 && start != w0 * s.share)) * size; };
+  float most = -__builtin_inff();
+  for (unsigned w = w0 + threadIdx.x; w <= worker; w += kThreads) most = fmaxf(most, piece(w)[ends]);
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  if (lane_id() == 0) tops[wave_id()] = most;
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < kWaves; ++n) most = fmaxf(most, tops[n]);
+  const float base = most == -__builtin_inff() ? 0.0f : most;
+  Vec<float, 4> x = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+  const unsigned d = lane_id() * 4;
+  for (unsigned w = w0 + wave_id(); w <= worker; w += kWaves) {
+    const float *p = piece(w);
+    const float f = __builtin_amdgcn_exp2f(p[ends] - base);
+    l += p[ends + 1] * f;
+    if (d < a.dim) x += *reinterpret_cast<const Vec<float, 4> *>(p + (unsigned long long)blockIdx.y * a.dim + d) * f;
+  }
+  if (lane_id() == 0) totals[wave_id()] = l;
+  *reinterpret_cast<Vec<float, 4> *>(&sums[wave_id()][d]) = x;
+  __syncthreads();
+  if (wave_id() != 0 || d >= a.dim) return;
+#pragma unroll
+  for (int n = 1; n < kWaves; ++n) {
+    l += totals[n];
+    x += *reinterpret_cast<const Vec<float, 4> *>(&sums[n][d]);
+  }
+  write_result<T>(a, s.request, head, d, x, most, l);
 }
 
 struct PagedAttention final : Operator {
   AttentionArgs a{};
   int32_t dtype;
-  unsigned requests;
+  size_t workspace() const override { return 2 * (size_t)a.workers * piece_floats(a.group, a.dim) * sizeof(float); }
   void record(Recorder &r) const override {
-    if (requests == 0 || a.heads == 0) return;
-    auto go = [&](auto element) { r.launch(&attention_kernel<decltype(element)>, a.heads, kThreads, a); r.launches.back().grid.y = requests; };
-    if (dtype == FC_F32) go(float{});
-    else if (dtype == FC_F16) go(_Float16{});
-    else go(__bf16{});
+    if (a.requests == 0 || a.group == 0) return;
+    AttentionArgs args = a;
+    args.pieces = reinterpret_cast<float *>(r.workspace);
+    auto by_dim = [&](auto element) {
+      using T = decltype(element);
+      auto go = [&](auto dim) {
+        constexpr int Dim = decltype(dim)::value;
+        if (a.dim == Dim) r.launch(&attention_kernel<T, Dim, true>, a.workers, kThreads, args);
+        else r.launch(&attention_kernel<T, Dim, false>, a.workers, kThreads, args);
+      };
+      if (a.dim <= 64) go(std::integral_constant<int, 64>{});
+      else if (a.dim <= 128) go(std::integral_constant<int, 128>{});
+      else go(std::integral_constant<int, 256>{});
+      r.launch(&attention_join_kernel<T>, a.workers, kThreads, args);
+      r.launches.back().grid.y = rows_of_piece(a.group);
+    };
+    if (dtype == FC_F32) by_dim(float{});
+    else if (dtype == FC_F16) by_dim(_Float16{});
+    else by_dim(__bf16{});
   }
   const char *name() const override { return "paged attention"; }
 };
@@ -128,12 +447,10 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   if (dim < 8 || dim % 8 || dim > (int64_t)kMostDim) return c.fail(FC_E_UNSUPPORTED, "heads have a multiple of 8 elements, at most 256").code();
   if (!std::isfinite(n.scale)) return c.fail(FC_E_ARG, "scale must be finite").code();
   if (n.window < 0) return c.fail(FC_E_ARG, "window must not be negative").code();
-  if (requests > 65535) return c.fail(FC_E_LIMIT, "more than 65535 requests").code();
   for (const fc_tensor *t : {&n.k_cache, &n.v_cache})
     if (pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16) return c.fail(FC_E_UNBOUND, "the caches' rows must be 16-byte aligned").code();
   auto op = std::make_unique<PagedAttention>();
   op->dtype = dtype;
-  op->requests = (unsigned)requests;
   AttentionArgs &a = op->a;
   a.q = static_cast<const char *>(n.q.ptr);
   a.k = static_cast<const char *>(n.k_cache.ptr);
@@ -154,14 +471,19 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   a.v_page = n.v_cache.stride[0];
   a.v_place = n.v_cache.stride[1];
   a.v_head = n.v_cache.stride[2];
-  a.heads = (unsigned)heads;
+  a.requests = (unsigned)requests;
+  a.kv_heads = (unsigned)kv;
   a.group = (unsigned)(heads / kv);
+  a.tiles = ceil_div(a.group, kColumns);
   a.dim = (unsigned)dim;
   a.page = (unsigned)page;
   a.pages = (unsigned)pages;
   a.width = (unsigned)n.table.shape[1];
   a.window = (unsigned)n.window;
-  a.scale = (float)n.scale;
+  a.scale = (float)(n.scale * (double)kLog2e);
+  const int units = device_compute_units();
+  a.workers = 4u * (unsigned)(units > 0 ? units : 256);
+  a.least_share = 1;
   out = std::move(op);
   return FC_OK;
 }
