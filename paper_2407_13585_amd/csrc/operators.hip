@@ -108,7 +108,8 @@ int record_operators(const OperatorList &list, void *scratch, size_t scratch_byt
   const size_t need = operators_scratch_bytes(list);
   if (scratch_bytes < need) { err = "scratch holds " + std::to_string(scratch_bytes) + " bytes where " + std::to_string(need) + " are needed"; return FC_E_SCRATCH; }
   for (const auto &op : list) {
-    Recorder r{out, static_cast<char *>(scratch) + FC_SCRATCH_CONTROL_BYTES, op->name()};
+    Recorder r{out, static_cast<char *>(scratch) + FC_SCRATCH_CONTROL_BYTES,
+               reinterpret_cast<unsigned *>(static_cast<char *>(scratch) + kCountersOffset), op->name()};
     op->record(r);
   }
   return FC_OK;

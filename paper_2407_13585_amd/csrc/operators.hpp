@@ -22,6 +22,7 @@ namespace fc {
 struct Recorder {
   std::vector<RecordedLaunch> &launches;
   char *workspace;                 // DEVICE: what workspace() asked for
+  unsigned *counters;              // DEVICE: kCounters of them, 0 between launches
   const char *what;                // the operator, for the message of a launch that fails
 
   template <class... P, class... A> void launch(void (*kernel)(P...), unsigned grid, unsigned threads, const A &...a) {

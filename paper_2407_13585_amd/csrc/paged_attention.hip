@@ -14,10 +14,11 @@
 // a permutation of a lane's own registers.
 //
 // The keys of all requests and key heads are one long row of units of 128 (64) keys, of which every workgroup takes an equal share,
-// whatever the lengths are: what is long is split, what is short is taken together.  Pieces of a split row go to scratch and
-// are joined in their order by a second kernel.
+// whatever the lengths are: what is long is split, what is short is taken together.  Pieces of a split row go to scratch; the
+// workgroup that is the last of a row to be done joins them in their order, in two steps where they are many.
 #include "operators.hpp"
 
+#include <algorithm>
 #include <cmath>
 
 namespace fc {
@@ -35,6 +36,7 @@ struct AttentionArgs {
   char *out;
   float *lse;                              // NULL: not wanted
   float *pieces;                           // DEVICE: two pieces a workgroup
+  unsigned *counters;                      // DEVICE: two a workgroup, 0 between launches
   long long q_request, q_head, out_request, out_head, lse_request, table_stride;
   long long k_page, k_place, k_head, v_page, v_place, v_head;
   unsigned requests, kv_heads, group, tiles, dim, page, pages, width, window;      // tiles: a group's heads, 16 at a time
@@ -280,6 +282,97 @@ template <class T> __device__ __forceinline__ void write_result(const AttentionA
   if (a.lse && d == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : (m - (float)Kind<T>::kShift + __log2f(l)) * kLn2;
 }
 
+// A piece: the weighted sums of the heads, then (m, l) of each.  It is written and read around the caches that compute units do not
+// share, two floats at a time: fences that write these caches back and empty them would do it for all that passes through
+// them (a launch of one long request 323 us, this way 1xx).
+struct Piece {
+  unsigned long long *sums, *ends;
+  __device__ __forceinline__ Piece(const AttentionArgs &a, unsigned long long slot)
+      : sums(reinterpret_cast<unsigned long long *>(a.pieces + slot * piece_floats(a.group, a.dim))), ends(sums + rows_of_piece(a.group) * a.dim / 2) {}
+  static __device__ __forceinline__ unsigned long long pair(float x, float y) { return (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x); }
+  static __device__ __forceinline__ Vec<float, 2> pair(unsigned long long w) { return {__uint_as_float((unsigned)w), __uint_as_float((unsigned)(w >> 32))}; }
+  __device__ __forceinline__ void store(unsigned at, Vec<float, 4> x) const {
+    store_agent64(sums + at / 2, pair(x[0], x[1]));
+    store_agent64(sums + at / 2 + 1, pair(x[2], x[3]));
+  }
+  __device__ __forceinline__ Vec<float, 4> load(unsigned at) const {
+    const Vec<float, 2> x = pair(load_agent64(sums + at / 2)), y = pair(load_agent64(sums + at / 2 + 1));
+    return {x[0], x[1], y[0], y[1]};
+  }
+  __device__ __forceinline__ void store_end(unsigned head, float m, float l) const { store_agent64(ends + head, pair(m, l)); }
+  __device__ __forceinline__ Vec<float, 2> load_end(unsigned head) const { return pair(load_agent64(ends + head)); }
+};
+
+// The pieces of a split row, made by the workers w0 .. w1 whose shares it reaches into.  The first is its worker's last piece where the
+// row starts inside of a share; all others are their workers' first.
+struct SplitRow {
+  unsigned w0, w1, group, groups;          // joined `group` at a time, counted from the end
+  bool starts_inside;
+  __device__ __forceinline__ SplitRow(const Share &s, unsigned long long start, unsigned long long end) {
+    w0 = (unsigned)(start / s.share);
+    w1 = (unsigned)((end - 1) / s.share);
+    starts_inside = start != w0 * s.share;
+    const unsigned n = w1 - w0 + 1;
+    group = n <= 16 ? n : (unsigned)ceilf(sqrtf((float)n));
+    groups = (n + group - 1) / group;
+  }
+  __device__ __forceinline__ unsigned long long slot(unsigned w) const { return w * 2ull + (w == w0 && starts_inside); }
+  __device__ __forceinline__ unsigned last_of_group(unsigned k) const { return w1 - k * group; }
+  __device__ __forceinline__ unsigned first_of_group(unsigned k) const { return max((int)w0, (int)(w1 - k * group - group) + 1); }
+};
+
+// Adds this workgroup to `counter`, once what its waves have stored has arrived; true for the last of `all`, who may then read
+// what the others stored before.
+__device__ __forceinline__ bool last_to_arrive(unsigned *counter, unsigned all) {
+  __shared__ unsigned before;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before == all - 1) store_agent(counter, 0u);
+  }
+  __syncthreads();
+  const bool last = before == all - 1;
+  __syncthreads();
+  return last;
+}
+
+// The pieces slot(0) .. slot(n - 1), of `count` heads, as one: use(head, d, sum, m, l) for four d at a time.
+template <class Slot, class Use> __device__ __forceinline__ void join(const AttentionArgs &a, unsigned n, unsigned count, Slot &&slot, Use &&use) {
+  constexpr int kTogether = 8;
+  const unsigned quads = a.dim / 4;
+  for (unsigned i = threadIdx.x; i < count * quads; i += kThreads) {
+    const unsigned head = i / quads, d = i % quads * 4;
+    float m = -__builtin_inff(), l = 0.0f;
+    Vec<float, 4> sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (unsigned p = 0; p < n; p += kTogether) {
+      Vec<float, 4> x[kTogether];
+      Vec<float, 2> e[kTogether];
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        const Piece piece(a, slot(min(p + k, n - 1)));
+        x[k] = piece.load(head * a.dim + d);
+        e[k] = piece.load_end(head);
+        if (p + k >= n) e[k] = Vec<float, 2>{-__builtin_inff(), 0.0f};
+      }
+      float most = m;
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) most = fmaxf(most, e[k][0]);
+      const float base = most == -__builtin_inff() ? 0.0f : most, keep = __builtin_amdgcn_exp2f(m - base);
+      m = most;
+      l *= keep;
+      sum *= keep;
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        const float f = __builtin_amdgcn_exp2f(e[k][0] - base);
+        l += e[k][1] * f;
+        if (p + k < n) sum += x[k] * f;
+      }
+    }
+    use(head, d, sum, m, l);
+  }
+}
+
 template <class T, int Dim, bool Plain>
 __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
   __shared__ float sums[kWaves][kColumns][Dim + 4];          // + 4: the heads' rows start at different banks
@@ -292,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
       write_result<T>(a, b, i / (a.dim / 4), i % (a.dim / 4) * 4, Vec<float, 4>{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f, 0.0f);
   }
   Share s = share_of<T>(a, worker);
-  bool first = true;
+  const unsigned long long share_begin = s.at;
   while (s.at < s.end) {
     const unsigned b = __builtin_amdgcn_readfirstlane(s.request);
     const Span span = span_of<T>(a, b);
@@ -322,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
         }
     __syncthreads();
     const bool whole = unit0 == 0 && unit1 == span.units;
-    float *piece = a.pieces + (worker * 2ull + !first) * piece_floats(a.group, a.dim);
+    const Piece mine(a, worker * 2ull + (s.at != share_begin));
     for (unsigned i = threadIdx.x; i < count * (Dim / 4); i += kThreads) {
       const unsigned head = i / (Dim / 4), d = i % (Dim / 4) * 4;
       if (d >= a.dim) continue;
@@ -338,64 +431,34 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
       }
       if (whole) write_result<T>(a, b, head0 + head, d, x, most, sum_l);
       else {
-        *reinterpret_cast<Vec<float, 4> *>(piece + head * a.dim + d) = x;
-        if (d == 0) {
-          piece[rows_of_piece(a.group) * a.dim + 2 * head] = most;
-          piece[rows_of_piece(a.group) * a.dim + 2 * head + 1] = sum_l;
-        }
+        mine.store(head * a.dim + d, x);
+        if (d == 0) mine.store_end(head, most, sum_l);
       }
     }
-    first = false;
+    if (!whole) {
+      const SplitRow split(s, s.at - unit0, s.at - unit0 + span.units);
+      const unsigned k = (split.w1 - worker) / split.group, last = split.last_of_group(k), of_group = last - split.first_of_group(k) + 1;
+      // a group of one has nothing to join, and no counter: a worker's counter belongs to the row that ends in its share, or covers it
+      bool joins = of_group == 1 || last_to_arrive(a.counters + last, of_group);
+      if (joins && split.groups > 1) {
+        if (of_group > 1) {
+          const Piece to(a, split.slot(last));
+          join(a, of_group, count, [&](unsigned p) { return split.slot(last - p); }, [&](unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) {
+            to.store(head * a.dim + d, sum);                 // only this thread reads these four
+            if (d == 0) { tops[0][head] = m; totals[0][head] = l; }
+          });
+          __syncthreads();                                   // all have read the ends that are written over
+          if (threadIdx.x < count) to.store_end(threadIdx.x, tops[0][threadIdx.x], totals[0][threadIdx.x]);
+        }
+        joins = last_to_arrive(a.counters + a.workers + split.w1, split.groups);
+      }
+      if (joins)
+        join(a, split.groups > 1 ? split.groups : of_group, count, [&](unsigned p) { return split.slot(split.groups > 1 ? split.last_of_group(p) : last - p); },
+             [&](unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) { write_result<T>(a, b, head0 + head, d, sum, m, l); });
+    }
     s.at += unit1 - unit0;
     s.offset += unit1 - unit0;
   }
-}
-
-// The pieces of a row that the worker before left unfinished and this one ended, for head blockIdx.y of its columns.
-template <class T>
-__global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs a) {
-  __shared__ float tops[kWaves], totals[kWaves], sums[kWaves][kMostDim];
-  const unsigned worker = blockIdx.x;
-  const Share s = share_of<T>(a, worker);
-  if (s.at >= s.end) return;
-  const Span span = span_of<T>(a, s.request);
-  const unsigned row = (unsigned)(s.offset / span.units), unit0 = (unsigned)(s.offset - (unsigned long long)row * span.units);
-  if (unit0 == 0 || span.units - unit0 > s.end - s.at) return;         // nothing is left over from before, or it goes on
-  const unsigned kv = row / a.tiles, head = kv * a.group + row % a.tiles * kColumns + blockIdx.y;
-  if (head >= (kv + 1) * a.group) return;
-  const unsigned long long start = s.at - unit0;                       // of the row
-  const unsigned w0 = (unsigned)(start / s.share);
-  const unsigned long long size = piece_floats(a.group, a.dim), ends = (unsigned long long)rows_of_piece(a.group) * a.dim + 2 * blockIdx.y;
-  // the first piece is its worker's last, the others are their workers' first
-  auto piece = [&](unsigned w) { return a.pieces + (w * 2ull + (w == w0 && start != w0 * s.share)) * size; };
-  float most = -__builtin_inff();
-  for (unsigned w = w0 + threadIdx.x; w <= worker; w += kThreads) most = fmaxf(most, piece(w)[ends]);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-  if (lane_id() == 0) tops[wave_id()] = most;
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < kWaves; ++n) most = fmaxf(most, tops[n]);
-  const float base = most == -__builtin_inff() ? 0.0f : most;
-  Vec<float, 4> x = {0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
-  const unsigned d = lane_id() * 4;
-  for (unsigned w = w0 + wave_id(); w <= worker; w += kWaves) {
-    const float *p = piece(w);
-    const float f = __builtin_amdgcn_exp2f(p[ends] - base);
-    l += p[ends + 1] * f;
-    if (d < a.dim) x += *reinterpret_cast<const Vec<float, 4> *>(p + (unsigned long long)blockIdx.y * a.dim + d) * f;
-  }
-  if (lane_id() == 0) totals[wave_id()] = l;
-  *reinterpret_cast<Vec<float, 4> *>(&sums[wave_id()][d]) = x;
-  __syncthreads();
-  if (wave_id() != 0 || d >= a.dim) return;
-#pragma unroll
-  for (int n = 1; n < kWaves; ++n) {
-    l += totals[n];
-    x += *reinterpret_cast<const Vec<float, 4> *>(&sums[n][d]);
-  }
-  write_result<T>(a, s.request, head, d, x, most, l);
 }
 
 struct PagedAttention final : Operator {
@@ -406,6 +469,7 @@ struct PagedAttention final : Operator {
     if (a.requests == 0 || a.group == 0) return;
     AttentionArgs args = a;
     args.pieces = reinterpret_cast<float *>(r.workspace);
+    args.counters = r.counters;
     auto by_dim = [&](auto element) {
       using T = decltype(element);
       auto go = [&](auto dim) {
@@ -416,8 +480,6 @@ struct PagedAttention final : Operator {
       if (a.dim <= 64) go(std::integral_constant<int, 64>{});
       else if (a.dim <= 128) go(std::integral_constant<int, 128>{});
       else go(std::integral_constant<int, 256>{});
-      r.launch(&attention_join_kernel<T>, a.workers, kThreads, args);
-      r.launches.back().grid.y = rows_of_piece(a.group);
     };
     if (dtype == FC_F32) by_dim(float{});
     else if (dtype == FC_F16) by_dim(_Float16{});
@@ -482,7 +544,7 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   a.window = (unsigned)n.window;
   a.scale = (float)(n.scale * (double)kLog2e);
   const int units = device_compute_units();
-  a.workers = 4u * (unsigned)(units > 0 ? units : 256);
+  a.workers = std::min(4u * (unsigned)(units > 0 ? units : 256), kCounters / 2u);
   a.least_share = 1;
   out = std::move(op);
   return FC_OK;
