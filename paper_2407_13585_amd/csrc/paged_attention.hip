@@ -41,7 +41,9 @@ struct AttentionArgs {
   long long k_page, k_place, k_head, v_page, v_place, v_head;
   unsigned requests, kv_heads, group, tiles, dim, page, pages, width, window;      // tiles: a group's heads, 16 at a time
   unsigned workers, least_share;
+  unsigned page_factor, page_shift;        // n / (page / 16) = n * page_factor >> page_shift, n below 2^30
   float scale;                             // times log2(e)
+  bool wide_q;                             // heads of q are aligned to 16 bytes
 };
 
 // What the types differ in.  kKeys: keys of a wave's step; kShift: the weights are held 2^kShift larger, which keeps the small ones
@@ -73,22 +75,31 @@ __device__ __forceinline__ void split(float p, _Float16 &high, _Float16 &low) {
   low = (_Float16)fmaxf(p - (float)high, 0x1p-24f);
 }
 
-// over the lanes of a head: lane, lane ^ 16, lane ^ 32, lane ^ 48
-__device__ __forceinline__ float column_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+// over the lanes of a head: lane, lane ^ 16, lane ^ 32, lane ^ 48.  Swapping a register's odd rows of 16 lanes with another's even ones,
+// or its upper half with the other's lower one, leaves the two values that belong together in the two.
+template <class F> __device__ __forceinline__ float over_column(float v, F &&f) {
+  auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
-__device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+__device__ __forceinline__ float column_max(float v) { return over_column(v, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float column_sum(float v) { return over_column(v, [](float x, float y) { return x + y; }); }
+
+// an element that this kernel does not write, for the whole wave: through the scalar unit, which has a counter of its own to wait for
+template <class T> __device__ __forceinline__ T load_scalar(const T *p) {
+  return *reinterpret_cast<const T __attribute__((address_space(4))) *>(reinterpret_cast<uintptr_t>(p));
 }
+
+// a value that all lanes have, in scalar registers
+__device__ __forceinline__ unsigned uniform(unsigned v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ unsigned long long uniform(unsigned long long v) { return (unsigned long long)uniform((unsigned)(v >> 32)) << 32 | uniform((unsigned)v); }
 
 // Keys of a request: [begin, end), from the step boundary `from` on in `units` units.
 struct Span {
   unsigned begin, end, from, units;
 };
-template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &a, unsigned b) {
-  const int length = a.lengths[b];
+template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &a, int length) {
   Span s;
   s.end = (unsigned)min((unsigned long long)max(length, 0), (unsigned long long)a.width * a.page);
   s.begin = a.window && length > 0 && (unsigned)length > a.window ? (unsigned)length - a.window : 0u;
@@ -99,41 +110,35 @@ template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &
 
 // This workgroup's share of all units: units [at, end) of the row, the first of them `offset` units into request `request`.
 struct Share {
-  unsigned long long at, end, offset, share;
-  unsigned request;
+  unsigned at, end, offset, share, request;
 };
 
 template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs &a, unsigned worker) {
-  __shared__ unsigned long long sums[kWaves], found_offset;
-  __shared__ unsigned found;
+  __shared__ unsigned sums[kWaves], found_offset, found;
   const unsigned rows = a.kv_heads * a.tiles, each = (a.requests + kThreads - 1) / kThreads;
   const unsigned b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
-  unsigned long long mine = 0;
-  for (unsigned b = b0; b < b1; ++b) mine += span_of<T>(a, b).units;
+  unsigned mine = 0;
+  for (unsigned b = b0; b < b1; ++b) mine += span_of<T>(a, a.lengths[b]).units;
   mine *= rows;
-  unsigned long long upto = mine;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const unsigned long long u = __shfl_up(upto, d);
-    if (lane_id() >= d) upto += u;
-  }
+  const unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)mine);
   if (lane_id() == kWave - 1) sums[wave_id()] = upto;
   __syncthreads();
-  unsigned long long before = 0, total = 0;
+  unsigned before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave_id()) before += sums[w];
     total += sums[w];
   }
   Share s;
-  s.share = max((total + a.workers - 1) / a.workers, (unsigned long long)a.least_share);
-  s.at = min(worker * s.share, total);
+  total = uniform(total);
+  s.share = max((total + a.workers - 1) / a.workers, a.least_share);
+  s.at = (unsigned)min((unsigned long long)worker * s.share, (unsigned long long)total);
   s.end = min(s.at + s.share, total);
   before += upto - mine;
   if (s.at >= before && s.at < before + mine) {
     unsigned b = b0;
     for (;; ++b) {
-      const unsigned long long here = (unsigned long long)span_of<T>(a, b).units * rows;
+      const unsigned here = span_of<T>(a, a.lengths[b]).units * rows;
       if (s.at < before + here) break;
       before += here;
     }
@@ -141,8 +146,8 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
     found_offset = s.at - before;
   }
   __syncthreads();
-  s.request = s.at < s.end ? found : 0u;
-  s.offset = s.at < s.end ? found_offset : 0ull;
+  s.request = s.at < s.end ? uniform(found) : 0u;
+  s.offset = s.at < s.end ? uniform(found_offset) : 0u;
   return s;
 }
 
@@ -150,93 +155,212 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
 __device__ __host__ __forceinline__ unsigned rows_of_piece(unsigned group) { return group < (unsigned)kColumns ? group : (unsigned)kColumns; }
 __device__ __host__ __forceinline__ unsigned long long piece_floats(unsigned group, unsigned dim) { return (unsigned long long)rows_of_piece(group) * (dim + 2); }
 
-template <class T, int Dim, bool Plain> struct Wave {
+// 16 (or 8) bytes of a lane through a descriptor; zeros where the offset lies past its end
+template <class T, int N> __device__ __forceinline__ Vec<T, N> load_buffer(__amdgpu_buffer_rsrc_t from, unsigned offset) {
+  if constexpr (sizeof(T) * N == 16)
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0));
+  else
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, 0));
+}
+
+// One wave's heads, and their state.  Even: every 16 keys from a multiple of 16 on lie on one page, and 16 keys of it span less than
+// 2^31 bytes: the page is then the wave's, its descriptor lies in scalar registers, and the lanes' offsets into 16 keys never change;
+// what is not there (other requests' keys, elements past D, pages outside the cache) is an offset or a descriptor that gives zeros.
+// Otherwise every lane looks its keys up.
+template <class T, int Dim, bool Even> struct Wave {
   static constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = 16 / sizeof(T);      // kWide: elements of 16 bytes
   static constexpr int kChunks = Dim / (4 * kWide);          // of K: 16 bytes of each of 4 lanes
   static constexpr int kW = Dim / 16;                        // d of a lane in V
   static constexpr int kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;  // ... in loads of 16 bytes at most
+  static constexpr unsigned kNothing = 0x80000000u;          // beyond every descriptor
   using Frag = Vec<T, kWide>;
   using Part = Vec<T, kPart>;
 
-  Frag q[kChunks];
+  // Where the keys of a step lie: the page of each 16 (Even), or of the lane's key of each 16.  a.pages: nowhere.
+  struct Where {
+    unsigned j0, page[kSub], place[kSub];
+  };
+
+  const AttentionArgs &a;
+  const Span s;
+  const int *table;
+  const T *k, *v;
+  unsigned r, g, k_at[kChunks], v_at[4][kParts];             // offsets in bytes into 16 keys (Even): of key r, and of keys 4g .. 4g+3
+  Frag q[kChunks], kf[kSub][kChunks];
+  Part vf[kSub][4][kParts];
   Acc o[kW];
   float m, l;
 
-  __device__ __forceinline__ void start(const AttentionArgs &a, const T *heads, unsigned count) {
-    const unsigned r = lane_id() & 15, g = lane_id() >> 4;
+  __device__ __forceinline__ Wave(const AttentionArgs &args, const Span &span, unsigned b, unsigned kv, unsigned head0, unsigned count)
+      : a(args), s(span), table(args.table + b * args.table_stride), k(reinterpret_cast<const T *>(args.k) + kv * args.k_head),
+        v(reinterpret_cast<const T *>(args.v) + kv * args.v_head), r(lane_id() & 15), g(lane_id() >> 4) {
+    const T *heads = reinterpret_cast<const T *>(a.q) + b * a.q_request + head0 * a.q_head;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       const unsigned d = (c * 4 + g) * kWide;
+      Frag f;
 #pragma unroll
-      for (int i = 0; i < kWide; ++i) q[c][i] = r < count && d + i < a.dim ? heads[r * a.q_head + d + i] : (T)0.0f;
+      for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
+      if (r < count && d < a.dim) {
+        const T *from = heads + r * a.q_head + d;
+        if (a.wide_q) f = load_vec<T, kWide>(from);
+        else {
+#pragma unroll
+          for (int i = 0; i < kWide; ++i) f[i] = from[i];
+        }
+      }
+      q[c] = f;
+      if constexpr (Even) k_at[c] = d < a.dim ? (unsigned)(r * a.k_place + d) * sizeof(T) : kNothing;
     }
+    if constexpr (Even)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int n = 0; n < kParts; ++n)
+          v_at[i][n] = r * kW + n * kPart < a.dim ? (unsigned)((4 * g + i) * a.v_place + r * kW + n * kPart) * sizeof(T) : kNothing;
 #pragma unroll
     for (int j = 0; j < kW; ++j) o[j] = Acc{0.0f, 0.0f, 0.0f, 0.0f};
     m = -__builtin_inff();
     l = 0.0f;
   }
 
-  // the keys j0 .. j0 + kKeys - 1, j0 a multiple of kKeys
-  __device__ __forceinline__ void step(const AttentionArgs &a, const Span &s, const int *table, const T *k, const T *v, unsigned j0) {
-    const unsigned r = lane_id() & 15, g = lane_id() >> 4;
-    Frag kf[kSub][kChunks];
-    Part vf[kSub][4][kParts];
-    bool there[kSub][4];                                     // the keys whose scores this lane gets
+  __device__ __forceinline__ bool inside(unsigned j) const { return j - s.begin < s.end - s.begin; }       // s.end > s.begin
+
+  __device__ __forceinline__ Where locate(unsigned j0) const {
+    Where w;
+    w.j0 = j0;
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
-      const unsigned j = j0 + 16 * u + r;
-      unsigned page = a.pages, place = 0;
-      if (j >= s.begin && j < s.end) {
-        const unsigned at = j / a.page;
-        page = (unsigned)table[at];
-        place = j - at * a.page;
-      }
-      const bool mine = page < a.pages;
-      const T *row = k + (mine ? page * a.k_page + place * a.k_place : 0ll);
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        const unsigned d = (c * 4 + g) * kWide;
-        Frag f;
-#pragma unroll
-        for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
-        if (mine && (Plain || d < a.dim)) f = load_vec<T, kWide>(row + d);
-        kf[u][c] = f;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned vp = __shfl(page, (int)(4 * g + i)), vo = __shfl(place, (int)(4 * g + i));
-        there[u][i] = vp < a.pages;
-        const T *values = v + (there[u][i] ? vp * a.v_page + vo * a.v_place : 0ll) + r * kW;
-#pragma unroll
-        for (int n = 0; n < kParts; ++n) {
-          Part f;
-#pragma unroll
-          for (int e = 0; e < kPart; ++e) f[e] = (T)0.0f;
-          if (there[u][i]) {
-            // heads have a multiple of 8 elements, a part 4 or 8: it is there as a whole or not at all
-            if (Plain || r * kW + n * kPart < a.dim) f = load_vec<T, kPart>(values + n * kPart);
-          }
-          vf[u][i][n] = f;
+      if constexpr (Even) {
+        const unsigned n = min(j0 + 16 * u, s.end - 1) / 16; // past the end: the last 16, whose page is then not looked at
+        const unsigned at = (unsigned)((unsigned long long)n * a.page_factor >> a.page_shift);
+        const unsigned page = (unsigned)load_scalar(table + at);
+        w.page[u] = j0 + 16 * u < s.end ? page : a.pages;
+        w.place[u] = 16 * n - at * a.page;
+      } else {
+        const unsigned j = j0 + 16 * u + r;
+        w.page[u] = a.pages;
+        w.place[u] = 0;
+        if (inside(j)) {
+          const unsigned at = j / a.page;
+          w.page[u] = (unsigned)table[at];
+          w.place[u] = j - at * a.page;
         }
       }
     }
-    float p[kSub][4], most = -__builtin_inff();
+    return w;
+  }
+
+  // whether every key of a step is there (Even)
+  __device__ __forceinline__ bool all_there(const Where &w) const {
+    bool all = w.j0 >= s.begin && w.j0 + kKeys <= s.end;
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) all &= w.page[u] < a.pages;
+    return all;
+  }
+
+  // descriptor of 16 keys: it ends behind the last that is there
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t keys_of(const T *cache, long long page_stride, long long place_stride, const Where &w, int u) const {
+    const bool there = w.page[u] < a.pages;
+    const T *base = cache + (there ? w.page[u] * page_stride + w.place[u] * place_stride : 0ll);
+    const unsigned keys = min(s.end - min(w.j0 + 16 * u, s.end), 16u);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(uniform((unsigned long long)base)), 0,
+                                             uniform(there ? keys * (unsigned)place_stride * (unsigned)sizeof(T) : 0u), 0x00027000);
+  }
+
+  __device__ __forceinline__ void load_keys(const Where &w) {
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) {
+      if constexpr (Even) {
+        const auto from = keys_of(k, a.k_page, a.k_place, w, u);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) kf[u][c] = load_buffer<T, kWide>(from, k_at[c]);
+      } else {
+        const bool mine = w.page[u] < a.pages;
+        const T *row = k + (mine ? w.page[u] * a.k_page + w.place[u] * a.k_place : 0ll);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          const unsigned d = (c * 4 + g) * kWide;
+          Frag f;
+#pragma unroll
+          for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
+          if (mine && d < a.dim) f = load_vec<T, kWide>(row + d);
+          kf[u][c] = f;
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void load_values(const Where &w) {
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) {
+      if constexpr (Even) {
+        const auto from = keys_of(v, a.v_page, a.v_place, w, u);
+        if (w.j0 + 16 * u >= s.begin) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, v_at[i][n]);
+        } else {                                             // keys before the window: a weight of zero would not do if they are not finite
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, w.j0 + 16 * u + 4 * g + i < s.begin ? kNothing : v_at[i][n]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned page = __shfl(w.page[u], (int)(4 * g + i)), place = __shfl(w.place[u], (int)(4 * g + i));
+          const bool mine = page < a.pages;
+          const T *row = v + (mine ? page * a.v_page + place * a.v_place : 0ll) + r * kW;
+#pragma unroll
+          for (int n = 0; n < kParts; ++n) {
+            Part f;
+#pragma unroll
+            for (int e = 0; e < kPart; ++e) f[e] = (T)0.0f;
+            // heads have a multiple of 8 elements, a part 4 or 8: it is there as a whole or not at all
+            if (mine && r * kW + n * kPart < a.dim) f = load_vec<T, kPart>(row + n * kPart);
+            vf[u][i][n] = f;
+          }
+        }
+      }
+    }
+  }
+
+  // weights of the keys of `w` from kf, the state brought up to them
+  __device__ __forceinline__ void weigh(const Where &w, float (&p)[kSub][4]) {
+    const bool all = Even && all_there(w);
+    float most = -__builtin_inff();
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
       Acc score = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) score = mma(kf[u][c], q[c], score);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[u][i] = there[u][i] ? score[i] * a.scale : -__builtin_inff();
-        most = fmaxf(most, p[u][i]);
-      }
+      for (int i = 0; i < 4; ++i) p[u][i] = score[i] * a.scale;
     }
+    if (!all) {
+#pragma unroll
+      for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned page = Even ? w.page[u] : (unsigned)__shfl(w.page[u], (int)(4 * g + i));
+          if (page >= a.pages || !inside(w.j0 + 16 * u + 4 * g + i)) p[u][i] = -__builtin_inff();
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kSub; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, p[u][i]);
     most = fmaxf(column_max(most), m);
     const float top = most == -__builtin_inff() ? 0.0f : most, base = top - (float)Kind<T>::kShift;
-    const float keep = __builtin_amdgcn_exp2f(m - top);
-    m = most;
-    l *= keep;
+    if (__any(most > m)) {                                   // of any head: the maxima settle after a few keys
+      const float keep = __builtin_amdgcn_exp2f(m - top);
+      m = most;
+      l *= keep;
+#pragma unroll
+      for (int j = 0; j < kW; ++j) o[j] *= keep;
+    }
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
 #pragma unroll
@@ -244,8 +368,10 @@ template <class T, int Dim, bool Plain> struct Wave {
         p[u][i] = __builtin_amdgcn_exp2f(p[u][i] - base);
         l += p[u][i];
       }
-#pragma unroll
-    for (int j = 0; j < kW; ++j) o[j] *= keep;
+  }
+
+  // the sums of vf with the weights
+  __device__ __forceinline__ void sum(const float (&p)[kSub][4]) {
     if constexpr (sizeof(T) == 2) {
       Vec<T, 8> high, low;
 #pragma unroll
@@ -268,6 +394,27 @@ template <class T, int Dim, bool Plain> struct Wave {
       for (int j = 0; j < kW; ++j)
         o[j] = mma(Vec<float, 4>{vf[0][0][j / kPart][j % kPart], vf[0][1][j / kPart][j % kPart], vf[0][2][j / kPart][j % kPart], vf[0][3][j / kPart][j % kPart]},
                    Vec<float, 4>{p[0][0], p[0][1], p[0][2], p[0][3]}, o[j]);
+    }
+  }
+
+  // The steps at j0, j0 + kUnit, .. below `end`.  The keys of the next step are asked for once this one's are used up, its values likewise,
+  // and the pages two steps ahead: steps past the end ask for nothing.
+  __device__ __forceinline__ void run(unsigned j0, unsigned end) {
+    if (j0 >= end) return;
+    Where now = locate(j0), next = locate(j0 + kUnit<T>);
+    load_keys(now);
+    load_values(now);
+    for (;;) {
+      Where after = locate(next.j0 + kUnit<T>);
+      float p[kSub][4];
+      weigh(now, p);
+      const bool more = next.j0 < end;
+      if (more) load_keys(next);
+      sum(p);
+      if (!more) break;
+      load_values(next);
+      now = next;
+      next = after;
     }
   }
 };
@@ -308,9 +455,9 @@ struct Piece {
 struct SplitRow {
   unsigned w0, w1, group, groups;          // joined `group` at a time, counted from the end
   bool starts_inside;
-  __device__ __forceinline__ SplitRow(const Share &s, unsigned long long start, unsigned long long end) {
-    w0 = (unsigned)(start / s.share);
-    w1 = (unsigned)((end - 1) / s.share);
+  __device__ __forceinline__ SplitRow(const Share &s, unsigned start, unsigned end) {
+    w0 = start / s.share;
+    w1 = (end - 1) / s.share;
     starts_inside = start != w0 * s.share;
     const unsigned n = w1 - w0 + 1;
     group = n <= 16 ? n : (unsigned)ceilf(sqrtf((float)n));
@@ -373,35 +520,28 @@ template <class Slot, class Use> __device__ __forceinline__ void join(const Atte
   }
 }
 
-template <class T, int Dim, bool Plain>
-__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
+template <class T, int Dim, bool Even>
+__global__ __launch_bounds__(kThreads, Dim == 64 ? 4 : Dim == 256 ? 1 : sizeof(T) == 2 ? 3 : 2) void attention_kernel(AttentionArgs a) {
   __shared__ float sums[kWaves][kColumns][Dim + 4];          // + 4: the heads' rows start at different banks
   __shared__ float tops[kWaves][kColumns], totals[kWaves][kColumns];
   const unsigned rows = a.kv_heads * a.tiles, worker = blockIdx.x;
   const unsigned r = lane_id() & 15, g = lane_id() >> 4;
   for (unsigned b = worker; b < a.requests; b += a.workers) {          // requests without a key
-    if (span_of<T>(a, b).units) continue;
+    if (span_of<T>(a, load_scalar(a.lengths + b)).units) continue;
     for (unsigned i = threadIdx.x; i < a.kv_heads * a.group * (a.dim / 4); i += kThreads)
       write_result<T>(a, b, i / (a.dim / 4), i % (a.dim / 4) * 4, Vec<float, 4>{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f, 0.0f);
   }
   Share s = share_of<T>(a, worker);
-  const unsigned long long share_begin = s.at;
+  const unsigned share_begin = s.at;
   while (s.at < s.end) {
-    const unsigned b = __builtin_amdgcn_readfirstlane(s.request);
-    const Span span = span_of<T>(a, b);
-    if (s.offset >= (unsigned long long)span.units * rows) { s.offset -= (unsigned long long)span.units * rows; ++s.request; continue; }
-    const unsigned row = __builtin_amdgcn_readfirstlane((unsigned)(s.offset / span.units)), unit0 = (unsigned)(s.offset - (unsigned long long)row * span.units);
-    const unsigned unit1 = (unsigned)min((unsigned long long)span.units, unit0 + (s.end - s.at));
+    const unsigned b = s.request;
+    const Span span = span_of<T>(a, load_scalar(a.lengths + b));
+    if (s.offset >= span.units * rows) { s.offset -= span.units * rows; ++s.request; continue; }
+    const unsigned row = s.offset / span.units, unit0 = s.offset - row * span.units, unit1 = min(span.units, unit0 + (s.end - s.at));
     const unsigned kv = row / a.tiles, head0 = kv * a.group + row % a.tiles * kColumns;
     const unsigned count = min((unsigned)kColumns, (kv + 1) * a.group - head0);
-    Wave<T, Dim, Plain> w;
-    w.start(a, reinterpret_cast<const T *>(a.q) + b * a.q_request + head0 * a.q_head, count);
-    const int *table = a.table + b * a.table_stride;
-    const T *k = reinterpret_cast<const T *>(a.k) + kv * a.k_head, *v = reinterpret_cast<const T *>(a.v) + kv * a.v_head;
-    for (unsigned unit = unit0; unit < unit1; ++unit) {
-      const unsigned j0 = span.from + unit * kUnit<T> + wave_id() * Kind<T>::kKeys;
-      if (j0 < span.end) w.step(a, span, table, k, v, j0);
-    }
+    Wave<T, Dim, Even> w(a, span, b, kv, head0, count);
+    w.run(span.from + unit0 * kUnit<T> + uniform((unsigned)wave_id()) * Kind<T>::kKeys, min(span.end, span.from + unit1 * kUnit<T>));
     const float total = column_sum(w.l);
     __syncthreads();                                         // the row before is read
     if (g == 0) { tops[wave_id()][r] = w.m; totals[wave_id()][r] = total; }
@@ -464,26 +604,34 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
 struct PagedAttention final : Operator {
   AttentionArgs a{};
   int32_t dtype;
+  bool even;
+  // calls f with the kernel for this call
+  template <class F> void with_kernel(F &&f) const {
+    auto by_dim = [&](auto element) {
+      using T = decltype(element);
+      auto by_form = [&](auto dim) { f(even ? &attention_kernel<T, decltype(dim)::value, true> : &attention_kernel<T, decltype(dim)::value, false>); };
+      if (a.dim <= 64) by_form(std::integral_constant<int, 64>{});
+      else if (a.dim <= 128) by_form(std::integral_constant<int, 128>{});
+      else by_form(std::integral_constant<int, 256>{});
+    };
+    if (dtype == FC_F32) by_dim(float{});
+    else if (dtype == FC_F16) by_dim(_Float16{});
+    else by_dim(__bf16{});
+  }
+  // as many workgroups as the device holds at once, but no more than there can be units
+  void settle_workers() {
+    unsigned resident = 0;
+    with_kernel([&](auto kernel) { resident = resident_workgroups(kernel, kThreads); });
+    a.workers = std::max(1u, std::min({resident ? resident : 512u, kCounters / 2u, most_units}));
+  }
+  unsigned most_units = 0;
   size_t workspace() const override { return 2 * (size_t)a.workers * piece_floats(a.group, a.dim) * sizeof(float); }
   void record(Recorder &r) const override {
     if (a.requests == 0 || a.group == 0) return;
     AttentionArgs args = a;
     args.pieces = reinterpret_cast<float *>(r.workspace);
     args.counters = r.counters;
-    auto by_dim = [&](auto element) {
-      using T = decltype(element);
-      auto go = [&](auto dim) {
-        constexpr int Dim = decltype(dim)::value;
-        if (a.dim == Dim) r.launch(&attention_kernel<T, Dim, true>, a.workers, kThreads, args);
-        else r.launch(&attention_kernel<T, Dim, false>, a.workers, kThreads, args);
-      };
-      if (a.dim <= 64) go(std::integral_constant<int, 64>{});
-      else if (a.dim <= 128) go(std::integral_constant<int, 128>{});
-      else go(std::integral_constant<int, 256>{});
-    };
-    if (dtype == FC_F32) by_dim(float{});
-    else if (dtype == FC_F16) by_dim(_Float16{});
-    else by_dim(__bf16{});
+    with_kernel([&](auto kernel) { r.launch(kernel, a.workers, kThreads, args); });
   }
   const char *name() const override { return "paged attention"; }
 };
@@ -542,10 +690,21 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   a.pages = (unsigned)pages;
   a.width = (unsigned)n.table.shape[1];
   a.window = (unsigned)n.window;
+  a.wide_q = common_alignment(n.q, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) == 16;
+  // the places of a page apart and in order, so that a descriptor's end tells what is there
+  op->even = page % 16 == 0 && std::min(a.k_place, a.v_place) >= dim && std::max(a.k_place, a.v_place) * 16 * size_of_dtype(dtype) < (int64_t)1 << 31;
+  if (op->even) {
+    // factor = ceil(2^(31 + s) / d), 2^s <= d: its error times n is below 2^(31 + s) for n below 2^30
+    const unsigned d = a.page / 16, s = 31u - (unsigned)__builtin_clz(d);
+    a.page_shift = 31 + s;
+    a.page_factor = (unsigned)(((1ull << a.page_shift) + d - 1) / d);
+  }
   a.scale = (float)(n.scale * (double)kLog2e);
-  const int units = device_compute_units();
-  a.workers = std::min(4u * (unsigned)(units > 0 ? units : 256), kCounters / 2u);
   a.least_share = 1;
+  const int64_t units = ceil_div((uint64_t)a.width * a.page, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;      // of a request: one more where a window starts inside
+  if (units * requests * kv * a.tiles > 0x7fffffff) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
+  op->most_units = (unsigned)(units * requests * kv * a.tiles);
+  op->settle_workers();
   out = std::move(op);
   return FC_OK;
 }
