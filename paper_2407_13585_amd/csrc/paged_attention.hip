@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr unsigned kMostDim = 256;
+constexpr unsigned kLongRow = 16;          // units
 constexpr int kColumns = 16;               // query heads of a group that are taken together
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
@@ -40,7 +41,7 @@ struct AttentionArgs {
   long long q_request, q_head, out_request, out_head, lse_request, table_stride;
   long long k_page, k_place, k_head, v_page, v_place, v_head;
   unsigned requests, kv_heads, group, tiles, dim, page, pages, width, window;      // tiles: a group's heads, 16 at a time
-  unsigned workers, least_share;
+  unsigned workers, streams;               // workgroups; as many of them as keep the memory busy with long rows
   unsigned page_factor, page_shift;        // n / (page / 16) = n * page_factor >> page_shift, n below 2^30
   float scale;                             // times log2(e)
   bool wide_q;                             // heads of q are aligned to 16 bytes
@@ -131,7 +132,10 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
   }
   Share s;
   total = uniform(total);
-  s.share = max((total + a.workers - 1) / a.workers, a.least_share);
+  // long rows keep a compute unit's memory pipe full with few workgroups, and the fewer they are the less is joined; short ones leave
+  // gaps that others fill
+  const unsigned workers = total >= kLongRow * a.requests * rows ? a.streams : a.workers;
+  s.share = max((total + workers - 1) / workers, 1u);
   s.at = (unsigned)min((unsigned long long)worker * s.share, (unsigned long long)total);
   s.end = min(s.at + s.share, total);
   before += upto - mine;
@@ -155,12 +159,14 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
 __device__ __host__ __forceinline__ unsigned rows_of_piece(unsigned group) { return group < (unsigned)kColumns ? group : (unsigned)kColumns; }
 __device__ __host__ __forceinline__ unsigned long long piece_floats(unsigned group, unsigned dim) { return (unsigned long long)rows_of_piece(group) * (dim + 2); }
 
+constexpr int kStream = 2;                 // of a load: read once, not worth keeping
+
 // 16 (or 8) bytes of a lane through a descriptor; zeros where the offset lies past its end
 template <class T, int N> __device__ __forceinline__ Vec<T, N> load_buffer(__amdgpu_buffer_rsrc_t from, unsigned offset) {
   if constexpr (sizeof(T) * N == 16)
-    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0));
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, kStream));
   else
-    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, 0));
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, kStream));
 }
 
 // One wave's heads, and their state.  Even: every 16 keys from a multiple of 16 on lie on one page, and 16 keys of it span less than
@@ -296,17 +302,11 @@ template <class T, int Dim, bool Even> struct Wave {
     for (int u = 0; u < kSub; ++u) {
       if constexpr (Even) {
         const auto from = keys_of(v, a.v_page, a.v_place, w, u);
-        if (w.j0 + 16 * u >= s.begin) {
+        // keys before the window give zeros: a weight of zero would not do where they are not finite
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, v_at[i][n]);
-        } else {                                             // keys before the window: a weight of zero would not do if they are not finite
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, w.j0 + 16 * u + 4 * g + i < s.begin ? kNothing : v_at[i][n]);
-        }
+          for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, w.j0 + 16 * u + 4 * g + i < s.begin ? kNothing : v_at[i][n]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -623,6 +623,9 @@ struct PagedAttention final : Operator {
     unsigned resident = 0;
     with_kernel([&](auto kernel) { resident = resident_workgroups(kernel, kThreads); });
     a.workers = std::max(1u, std::min({resident ? resident : 512u, kCounters / 2u, most_units}));
+    // a wave's step reads 128 D bytes: 16 kB under way for each of four waves are enough
+    const int units = device_compute_units();
+    a.streams = even ? std::min(a.workers, (units > 0 ? (unsigned)units : 256u) * ceil_div(128, a.dim)) : a.workers;
   }
   unsigned most_units = 0;
   size_t workspace() const override { return 2 * (size_t)a.workers * piece_floats(a.group, a.dim) * sizeof(float); }
@@ -700,7 +703,6 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
     a.page_factor = (unsigned)(((1ull << a.page_shift) + d - 1) / d);
   }
   a.scale = (float)(n.scale * (double)kLog2e);
-  a.least_share = 1;
   const int64_t units = ceil_div((uint64_t)a.width * a.page, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;      // of a request: one more where a window starts inside
   if (units * requests * kv * a.tiles > 0x7fffffff) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
   op->most_units = (unsigned)(units * requests * kv * a.tiles);
