@@ -10,7 +10,7 @@
 //                       the keys 4g .. 4g+3 of every 16
 //   outputs = V^T p^T   rows: d,        columns: heads, sum over keys
 // The sum over keys takes them in any order, so a lane passes the weights on where the scores left them, and reads the values of
-// just these keys, d = W r .. W r + W-1 (W = D / 16) of each: rows of V are read whole and in order, and the transposition is
+// just these keys, 16 bytes of each at a time, the 16 lanes of a key side by side: rows of V are read in order, and the transposition is
 // a permutation of a lane's own registers.
 //
 // The keys of all requests and key heads are one long row of units of 128 (64) keys, of which every workgroup takes an equal share,
@@ -159,14 +159,16 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
 __device__ __host__ __forceinline__ unsigned rows_of_piece(unsigned group) { return group < (unsigned)kColumns ? group : (unsigned)kColumns; }
 __device__ __host__ __forceinline__ unsigned long long piece_floats(unsigned group, unsigned dim) { return (unsigned long long)rows_of_piece(group) * (dim + 2); }
 
-constexpr int kStream = 2;                 // of a load: read once, not worth keeping
+// Hints of a load: kept, or read once and not worth keeping.  A key's line is read in two instructions, which keeps it; a value's in one, and
+// the way past the caches is the faster (64 ragged requests 212 us, 193 this way, 201 with the keys past the caches too).
+constexpr int kKept = 0, kStream = 2;
 
 // 16 (or 8) bytes of a lane through a descriptor; zeros where the offset lies past its end
-template <class T, int N> __device__ __forceinline__ Vec<T, N> load_buffer(__amdgpu_buffer_rsrc_t from, unsigned offset) {
+template <int Hint, class T, int N> __device__ __forceinline__ Vec<T, N> load_buffer(__amdgpu_buffer_rsrc_t from, unsigned offset) {
   if constexpr (sizeof(T) * N == 16)
-    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, kStream));
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, Hint));
   else
-    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, kStream));
+    return __builtin_bit_cast(Vec<T, N>, __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, Hint));
 }
 
 // One wave's heads, and their state.  Even: every 16 keys from a multiple of 16 on lie on one page, and 16 keys of it span less than
@@ -176,7 +178,7 @@ template <class T, int N> __device__ __forceinline__ Vec<T, N> load_buffer(__amd
 template <class T, int Dim, bool Even> struct Wave {
   static constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = 16 / sizeof(T);      // kWide: elements of 16 bytes
   static constexpr int kChunks = Dim / (4 * kWide);          // of K: 16 bytes of each of 4 lanes
-  static constexpr int kW = Dim / 16;                        // d of a lane in V
+  static constexpr int kW = Dim / 16;                        // d of a lane in V: parts n of kPart from (16 n + r) kPart on
   static constexpr int kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;  // ... in loads of 16 bytes at most
   static constexpr unsigned kNothing = 0x80000000u;          // beyond every descriptor
   using Frag = Vec<T, kWide>;
@@ -223,12 +225,15 @@ template <class T, int Dim, bool Even> struct Wave {
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int n = 0; n < kParts; ++n)
-          v_at[i][n] = r * kW + n * kPart < a.dim ? (unsigned)((4 * g + i) * a.v_place + r * kW + n * kPart) * sizeof(T) : kNothing;
+          v_at[i][n] = (16 * n + r) * kPart < a.dim ? (unsigned)((4 * g + i) * a.v_place + (16 * n + r) * kPart) * sizeof(T) : kNothing;
 #pragma unroll
     for (int j = 0; j < kW; ++j) o[j] = Acc{0.0f, 0.0f, 0.0f, 0.0f};
     m = -__builtin_inff();
     l = 0.0f;
   }
+
+  // which d of its head o[j][i] is
+  __device__ __forceinline__ unsigned d_of(int i, int j) const { return (j / kPart * 16 + 4 * g + i) * kPart + j % kPart; }
 
   __device__ __forceinline__ bool inside(unsigned j) const { return j - s.begin < s.end - s.begin; }       // s.end > s.begin
 
@@ -280,7 +285,7 @@ template <class T, int Dim, bool Even> struct Wave {
       if constexpr (Even) {
         const auto from = keys_of(k, a.k_page, a.k_place, w, u);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) kf[u][c] = load_buffer<T, kWide>(from, k_at[c]);
+        for (int c = 0; c < kChunks; ++c) kf[u][c] = load_buffer<kKept, T, kWide>(from, k_at[c]);
       } else {
         const bool mine = w.page[u] < a.pages;
         const T *row = k + (mine ? w.page[u] * a.k_page + w.place[u] * a.k_place : 0ll);
@@ -306,20 +311,20 @@ template <class T, int Dim, bool Even> struct Wave {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<T, kPart>(from, w.j0 + 16 * u + 4 * g + i < s.begin ? kNothing : v_at[i][n]);
+          for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_buffer<kStream, T, kPart>(from, w.j0 + 16 * u + 4 * g + i < s.begin ? kNothing : v_at[i][n]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const unsigned page = __shfl(w.page[u], (int)(4 * g + i)), place = __shfl(w.place[u], (int)(4 * g + i));
           const bool mine = page < a.pages;
-          const T *row = v + (mine ? page * a.v_page + place * a.v_place : 0ll) + r * kW;
+          const T *row = v + (mine ? page * a.v_page + place * a.v_place : 0ll) + r * kPart;
 #pragma unroll
           for (int n = 0; n < kParts; ++n) {
             Part f;
 #pragma unroll
             for (int e = 0; e < kPart; ++e) f[e] = (T)0.0f;
             // heads have a multiple of 8 elements, a part 4 or 8: it is there as a whole or not at all
-            if (mine && r * kW + n * kPart < a.dim) f = load_vec<T, kPart>(row + n * kPart);
+            if (mine && (16 * n + r) * kPart < a.dim) f = load_vec<T, kPart>(row + n * 16 * kPart);
             vf[u][i][n] = f;
           }
         }
@@ -551,7 +556,7 @@ __global__ __launch_bounds__(kThreads, Dim == 64 ? 4 : Dim == 256 ? 1 : sizeof(T
 #pragma unroll
         for (int j = 0; j < Dim / 16; j += 4) {
           Vec<float, 4> x = {w.o[j][i], w.o[j + 1][i], w.o[j + 2][i], w.o[j + 3][i]};
-          *reinterpret_cast<Vec<float, 4> *>(&sums[wave_id()][r][(4 * g + i) * (Dim / 16) + j]) = x;
+          *reinterpret_cast<Vec<float, 4> *>(&sums[wave_id()][r][w.d_of(i, j)]) = x;
         }
     __syncthreads();
     const bool whole = unit0 == 0 && unit1 == span.units;
