@@ -407,7 +407,7 @@ typedef struct fc_head_norm_rope_grad {
  *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
  * A request without keys gets zeros and -inf.  What lies in the pages past a request's length is not looked at, whatever it holds. */
 typedef struct fc_paged_attention {
-  fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256 */
+  fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
   fc_tensor k_cache;      /* [pages, P, Hk, D], in any order of strides with D innermost; rows 16-byte aligned */
   fc_tensor v_cache;
   fc_tensor table;        /* i32 [B, W] */

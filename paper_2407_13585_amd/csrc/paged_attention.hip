@@ -44,7 +44,6 @@ struct AttentionArgs {
   unsigned workers, streams;               // workgroups; as many of them as keep the memory busy with long rows
   unsigned page_factor, page_shift;        // n / (page / 16) = n * page_factor >> page_shift, n below 2^30
   float scale;                             // times log2(e)
-  bool wide_q;                             // heads of q are aligned to 16 bytes
 };
 
 // What the types differ in.  kKeys: keys of a wave's step; kShift: the weights are held 2^kShift larger, which keeps the small ones
@@ -209,14 +208,7 @@ template <class T, int Dim, bool Even> struct Wave {
       Frag f;
 #pragma unroll
       for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
-      if (r < count && d < a.dim) {
-        const T *from = heads + r * a.q_head + d;
-        if (a.wide_q) f = load_vec<T, kWide>(from);
-        else {
-#pragma unroll
-          for (int i = 0; i < kWide; ++i) f[i] = from[i];
-        }
-      }
+      if (r < count && d < a.dim) f = load_vec<T, kWide>(heads + r * a.q_head + d);
       q[c] = f;
       if constexpr (Even) k_at[c] = d < a.dim ? (unsigned)(r * a.k_place + d) * sizeof(T) : kNothing;
     }
@@ -387,12 +379,15 @@ template <class T, int Dim, bool Even> struct Wave {
         low[e] = rest;
       }
 #pragma unroll
-      for (int j = 0; j < kW; ++j) {
-        Vec<T, 8> values;
+      for (int n = 0; n < kParts; ++n) {
+        const Part v0 = vf[0][0][n], v1 = vf[0][1][n], v2 = vf[0][2][n], v3 = vf[0][3][n], v4 = vf[1][0][n], v5 = vf[1][1][n], v6 = vf[1][2][n], v7 = vf[1][3][n];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) values[e] = vf[e / 4][e % 4][j / kPart][j % kPart];
-        o[j] = mma(values, high, o[j]);
-        o[j] = mma(values, low, o[j]);
+        for (int e = 0; e < kPart; ++e) {
+          const Vec<T, 8> values = {v0[e], v1[e], v2[e], v3[e], v4[e], v5[e], v6[e], v7[e]};
+          Acc &sums = o[n * kPart + e];
+          sums = mma(values, high, sums);
+          sums = mma(values, low, sums);
+        }
       }
     } else {
 #pragma unroll
@@ -665,8 +660,9 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   if (dim < 8 || dim % 8 || dim > (int64_t)kMostDim) return c.fail(FC_E_UNSUPPORTED, "heads have a multiple of 8 elements, at most 256").code();
   if (!std::isfinite(n.scale)) return c.fail(FC_E_ARG, "scale must be finite").code();
   if (n.window < 0) return c.fail(FC_E_ARG, "window must not be negative").code();
-  for (const fc_tensor *t : {&n.k_cache, &n.v_cache})
-    if (pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16) return c.fail(FC_E_UNBOUND, "the caches' rows must be 16-byte aligned").code();
+  for (const fc_tensor *t : {&n.q, &n.k_cache, &n.v_cache})
+    if (requests && pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16)
+      return c.fail(FC_E_UNBOUND, "the rows of q and of the caches must be 16-byte aligned").code();
   auto op = std::make_unique<PagedAttention>();
   op->dtype = dtype;
   AttentionArgs &a = op->a;
@@ -698,7 +694,6 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   a.pages = (unsigned)pages;
   a.width = (unsigned)n.table.shape[1];
   a.window = (unsigned)n.window;
-  a.wide_q = common_alignment(n.q, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) == 16;
   // the places of a page apart and in order, so that a descriptor's end tells what is there
   op->even = page % 16 == 0 && std::min(a.k_place, a.v_place) >= dim && std::max(a.k_place, a.v_place) * 16 * size_of_dtype(dtype) < (int64_t)1 << 31;
   if (op->even) {

@@ -152,6 +152,7 @@ REFUSED = [
     ("FC_E_UNSUPPORTED", lambda: attention(dim=264)),
     ("FC_E_UNSUPPORTED", lambda: attention(dim=60)),
     ("FC_E_UNBOUND", lambda: attention(k_cache=T("bfloat16", 9, 16, 2, 64, ptr=0x20000008))),
+    ("FC_E_UNBOUND", lambda: attention(q=T("bfloat16", 3, 4, 64, ptr=0x20000008))),
     ("FC_E_UNBOUND", lambda: attention(v_cache=T("bfloat16", 9, 16, 2, 64, stride=(2052, 128, 64, 1)))),
     ("FC_E_UNBOUND", lambda: attention(table=T("int32", 3, 8, ptr=0))),
 ]
