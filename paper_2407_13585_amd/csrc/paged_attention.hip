@@ -101,7 +101,7 @@ struct Span {
 };
 template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &a, int length) {
   Span s;
-  s.end = (unsigned)min((unsigned long long)max(length, 0), (unsigned long long)a.width * a.page);
+  s.end = a.pages ? (unsigned)min((unsigned long long)max(length, 0), (unsigned long long)a.width * a.page) : 0u;
   s.begin = a.window && length > 0 && (unsigned)length > a.window ? (unsigned)length - a.window : 0u;
   s.from = s.begin / Kind<T>::kKeys * Kind<T>::kKeys;
   s.units = s.end > s.begin ? (s.end - s.from + kUnit<T> - 1) / kUnit<T> : 0u;
@@ -195,6 +195,7 @@ template <class T, int Dim, bool Even> struct Wave {
   unsigned r, g, k_at[kChunks], v_at[4][kParts];             // offsets in bytes into 16 keys (Even): of key r, and of keys 4g .. 4g+3
   Frag q[kChunks], kf[kSub][kChunks];
   Part vf[kSub][4][kParts];
+  bool there[kSub][4];                                       // the keys 4g + i of vf (not Even)
   Acc o[kW];
   float m, l;
 
@@ -279,16 +280,13 @@ template <class T, int Dim, bool Even> struct Wave {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) kf[u][c] = load_buffer<kKept, T, kWide>(from, k_at[c]);
       } else {
+        // what is not there reads a place that is, and is put right where it is used: nothing has to wait here
         const bool mine = w.page[u] < a.pages;
         const T *row = k + (mine ? w.page[u] * a.k_page + w.place[u] * a.k_place : 0ll);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
           const unsigned d = (c * 4 + g) * kWide;
-          Frag f;
-#pragma unroll
-          for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
-          if (mine && d < a.dim) f = load_vec<T, kWide>(row + d);
-          kf[u][c] = f;
+          kf[u][c] = load_vec<T, kWide>(row + (d < a.dim ? d : 0u));
         }
       }
     }
@@ -309,24 +307,51 @@ template <class T, int Dim, bool Even> struct Wave {
         for (int i = 0; i < 4; ++i) {
           const unsigned page = __shfl(w.page[u], (int)(4 * g + i)), place = __shfl(w.place[u], (int)(4 * g + i));
           const bool mine = page < a.pages;
-          const T *row = v + (mine ? page * a.v_page + place * a.v_place : 0ll) + r * kPart;
+          there[u][i] = mine;
+          const T *row = v + (mine ? page * a.v_page + place * a.v_place : 0ll);
 #pragma unroll
-          for (int n = 0; n < kParts; ++n) {
-            Part f;
-#pragma unroll
-            for (int e = 0; e < kPart; ++e) f[e] = (T)0.0f;
-            // heads have a multiple of 8 elements, a part 4 or 8: it is there as a whole or not at all
-            if (mine && (16 * n + r) * kPart < a.dim) f = load_vec<T, kPart>(row + n * 16 * kPart);
-            vf[u][i][n] = f;
-          }
+          for (int n = 0; n < kParts; ++n) vf[u][i][n] = load_vec<T, kPart>(row + ((16 * n + r) * kPart < a.dim ? (16 * n + r) * kPart : 0u));
         }
       }
     }
   }
 
+  // Zeros for what load_keys and load_values read in place of what is not there (not Even): keys past D of a head, whose query is zero
+  // there, and the values of keys that have none, whose weight is, would be more than nothing where they are not finite.  Elements
+  // past D of the values make sums that nobody reads.
+  __device__ __forceinline__ void clear_keys() {
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      if ((c * 4 + 4) * kWide > (int)a.dim)
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+          for (int i = 0; i < kWide; ++i) kf[u][c][i] = (c * 4 + g) * kWide < a.dim ? kf[u][c][i] : (T)0.0f;
+  }
+  __device__ __forceinline__ void clear_values() {
+#pragma unroll
+    for (int u = 0; u < kSub; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int n = 0; n < kParts; ++n)
+#pragma unroll
+          for (int e = 0; e < kPart; ++e) vf[u][i][n][e] = there[u][i] ? vf[u][i][n][e] : (T)0.0f;
+  }
+
   // weights of the keys of `w` from kf, the state brought up to them
   __device__ __forceinline__ void weigh(const Where &w, float (&p)[kSub][4]) {
-    const bool all = Even && all_there(w);
+    bool all = Even && all_there(w);
+    if constexpr (!Even) {
+      clear_keys();
+      bool mine = true;
+#pragma unroll
+      for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine &= there[u][i];
+      all = __all(mine);
+      if (!all) clear_values();
+    }
     float most = -__builtin_inff();
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
@@ -341,8 +366,8 @@ template <class T, int Dim, bool Even> struct Wave {
       for (int u = 0; u < kSub; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const unsigned page = Even ? w.page[u] : (unsigned)__shfl(w.page[u], (int)(4 * g + i));
-          if (page >= a.pages || !inside(w.j0 + 16 * u + 4 * g + i)) p[u][i] = -__builtin_inff();
+          const bool mine = Even ? w.page[u] < a.pages && inside(w.j0 + 16 * u + 4 * g + i) : there[u][i];
+          if (!mine) p[u][i] = -__builtin_inff();
         }
     }
 #pragma unroll
@@ -431,7 +456,7 @@ template <class T> __device__ __forceinline__ void write_result(const AttentionA
 
 // A piece: the weighted sums of the heads, then (m, l) of each.  It is written and read around the caches that compute units do not
 // share, two floats at a time: fences that write these caches back and empty them would do it for all that passes through
-// them (a launch of one long request 323 us, this way 1xx).
+// them (a launch of one long request 323 us, this way 122).
 struct Piece {
   unsigned long long *sums, *ends;
   __device__ __forceinline__ Piece(const AttentionArgs &a, unsigned long long slot)
@@ -521,7 +546,7 @@ template <class Slot, class Use> __device__ __forceinline__ void join(const Atte
 }
 
 template <class T, int Dim, bool Even>
-__global__ __launch_bounds__(kThreads, Dim == 64 ? 4 : Dim == 256 ? 1 : sizeof(T) == 2 ? 3 : 2) void attention_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, Dim == 256 ? 1 : Dim == 128 ? (Even && sizeof(T) == 2 ? 3 : 2) : Even ? 4 : 3) void attention_kernel(AttentionArgs a) {
   __shared__ float sums[kWaves][kColumns][Dim + 4];          // + 4: the heads' rows start at different banks
   __shared__ float tops[kWaves][kColumns], totals[kWaves][kColumns];
   const unsigned rows = a.kv_heads * a.tiles, worker = blockIdx.x;
