@@ -31,18 +31,12 @@ struct HeadsArgs {
   long long angle_stride, position_stride;
   long long k_page, k_place, v_page, v_place, v_head;     // strides of the caches
   unsigned tokens, heads[3];        // of q, k, v
-  unsigned dim, half, page, pages;  // half: R / 2
+  unsigned dim, half, page, places; // half: R / 2; places: of the cache
   unsigned axes, angles;            // rows of positions and of cos_sin
   unsigned lanes_log2, per_wave;    // lanes of a row; heads of a token that a wave takes
   float eps;
   bool wide_angles;                 // rows of cos_sin are aligned for packs
 };
-
-// by value: a choice between two places would put both into memory
-__device__ __forceinline__ float either(bool first, float a, float b) { return first ? a : b; }
-__device__ __forceinline__ Rows either(bool first, Rows a, Rows b) {
-  return {first ? a.ptr : b.ptr, first ? a.token : b.token, first ? a.head : b.head};
-}
 
 // Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.
 template <int V, bool Interleaved> struct Place {
@@ -57,30 +51,40 @@ template <int V, bool Interleaved> struct Place {
   }
 };
 
-// zeros where there is nothing, or where `live` is false
-template <class T, int V, bool Interleaved>
-__device__ __forceinline__ void load_row(const T *row, const Place<V, Interleaved> &p, bool live, float (&x)[2][V]) {
+// A lane's part of a row as it lies in memory.
+template <class T, int V> struct Packs {
   Vec<T, V> a, b;
+};
+
+// zeros where there is nothing, or where `live` is false
+template <bool Stream, class T, int V, bool Interleaved>
+__device__ __forceinline__ Packs<T, V> load_packs(const T *row, const Place<V, Interleaved> &p, bool live) {
+  Packs<T, V> x;
 #pragma unroll
-  for (int i = 0; i < V; ++i) a[i] = b[i] = (T)0.0f;
+  for (int i = 0; i < V; ++i) x.a[i] = x.b[i] = (T)0.0f;
   if (p.any && live) {
-    a = load_vec<T, V>(row + p.at[0]);
-    b = load_vec<T, V>(row + p.at[1]);
+    x.a = load_vec<T, V, Stream>(row + p.at[0]);
+    x.b = load_vec<T, V, Stream>(row + p.at[1]);
   }
+  return x;
+}
+
+// its pairs: the i-th is (x[0][i], x[1][i])
+template <class T, int V, bool Interleaved> __device__ __forceinline__ void unpack(const Packs<T, V> &w, const Place<V, Interleaved> &, float (&x)[2][V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     if constexpr (Interleaved) {    // also behind the rotated part: the two packs follow each other there
       const int e = 2 * i, o = 2 * i + 1;
-      x[0][i] = e < V ? (float)a[e % V] : (float)b[e % V];
-      x[1][i] = o < V ? (float)a[o % V] : (float)b[o % V];
+      x[0][i] = e < V ? (float)w.a[e % V] : (float)w.b[e % V];
+      x[1][i] = o < V ? (float)w.a[o % V] : (float)w.b[o % V];
     } else {
-      x[0][i] = (float)a[i];
-      x[1][i] = (float)b[i];
+      x[0][i] = (float)w.a[i];
+      x[1][i] = (float)w.b[i];
     }
   }
 }
 
-template <class T, int V, bool Interleaved>
+template <bool Stream, class T, int V, bool Interleaved>
 __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p, const float (&x)[2][V]) {
   if (!p.any) return;
   Vec<T, V> a, b;
@@ -95,8 +99,8 @@ __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p
       b[i] = (T)x[1][i];
     }
   }
-  store_vec<T, V>(row + p.at[0], a);
-  store_vec<T, V>(row + p.at[1], b);
+  store_vec<T, V, Stream>(row + p.at[0], a);
+  store_vec<T, V, Stream>(row + p.at[1], b);
 }
 
 // Cosines and sines of the pairs of this lane at token t: 1 and 0 where nothing is turned, NaN where the table has no row.
@@ -144,16 +148,39 @@ __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, I
   }
 }
 
-template <class T, int V, bool Interleaved>
-__device__ __forceinline__ void load_weight(const HeadsArgs &a, int which, const Place<V, Interleaved> &p, float (&w)[2][V]) {
-  const bool any = a.weight[which] != nullptr;
-  load_row<T, V, Interleaved>(static_cast<const T *>(a.weight[which]), p, any, w);
+// by value: a choice between two places would put both into memory
+template <class T, int V> __device__ __forceinline__ Packs<T, V> either(bool first, const Packs<T, V> &x, const Packs<T, V> &y) {
+  Packs<T, V> w;
+  w.a = first ? x.a : y.a;
+  w.b = first ? x.b : y.b;
+  return w;
+}
+__device__ __forceinline__ Rows either(bool first, Rows a, Rows b) {
+  return {first ? a.ptr : b.ptr, first ? a.token : b.token, first ? a.head : b.head};
+}
+template <class T> __device__ __forceinline__ T *row_of(Rows rows, unsigned t, unsigned head) {
+  return reinterpret_cast<T *>(rows.ptr) + t * rows.token + head * rows.head;
+}
+
+// ones where there is no weight
+template <class T, int V, bool Interleaved> __device__ __forceinline__ Packs<T, V> load_weight(const void *weight, const Place<V, Interleaved> &p) {
+  Packs<T, V> w = load_packs<false>(static_cast<const T *>(weight), p, weight != nullptr);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    w[0][i] = any ? w[0][i] : 1.0f;
-    w[1][i] = any ? w[1][i] : 1.0f;
+    w.a[i] = weight ? w.a[i] : (T)1.0f;
+    w.b[i] = weight ? w.b[i] : (T)1.0f;
   }
+  return w;
 }
+
+// What a wave does: the heads [first, end) of the tokens blockIdx.x * kWaves + wave, .. ; q, k and v heads are numbered in one row.  A row is
+// read while the one before is worked on.
+struct Turn {
+  bool live, is_q, is_v;
+  unsigned head;
+  __device__ __forceinline__ Turn(const HeadsArgs &a, unsigned h, unsigned end)
+      : live(h < end), is_q(h < a.heads[0]), is_v(h >= a.heads[0] + a.heads[1]), head(is_q ? h : is_v ? h - a.heads[0] - a.heads[1] : h - a.heads[0]) {}
+};
 
 template <int V> __device__ __forceinline__ float sum_of_products(const float (&x)[2][V], const float (&y)[2][V]) {
   float s = 0.0f;
@@ -162,49 +189,47 @@ template <int V> __device__ __forceinline__ float sum_of_products(const float (&
   return s;
 }
 
-// The units of work: a token with per_wave of its heads (q, k and v numbered in one row), a wave each.
-template <class T, int V, bool Interleaved>
+template <class T, int V, bool Interleaved, bool Stream>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
   const Place<V, Interleaved> p(a.dim, a.half, chunk);
-  float wq[2][V], wk[2][V];
-  load_weight<T, V, Interleaved>(a, 0, p, wq);
-  load_weight<T, V, Interleaved>(a, 1, p, wk);
-  const unsigned heads = a.heads[0] + a.heads[1] + a.heads[2], parts = (heads + a.per_wave - 1) / a.per_wave;
-  const unsigned long long units = (unsigned long long)a.tokens * parts;
+  const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
+  const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1] + a.heads[2]);
   const float by_dim = 1.0f / (float)a.dim;
-  for (unsigned long long u = (unsigned long long)blockIdx.x * kWaves + wave_id(); u < units; u += (unsigned long long)gridDim.x * kWaves) {
-    const unsigned t = (unsigned)(u / parts), h0 = (unsigned)(u % parts) * a.per_wave;
+  auto load = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, either(n.is_v, a.v, a.k)), t, n.head), p, n.live); };
+  for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
+    auto next = load(Turn(a, first + row_of_wave, end), t);
     float c[V], s[V];
     load_angles(a, p, t, c, s);
     const long long slot = a.slots ? a.slots[t] : 0;
-    const bool stored = !a.slots || (unsigned long long)slot < (unsigned long long)a.pages * a.page;
-    const unsigned page = a.slots && stored ? (unsigned)(slot / a.page) : 0u, place = a.slots && stored ? (unsigned)(slot - (long long)page * a.page) : 0u;
-    for (unsigned h = h0 + row_of_wave; h < min(h0 + a.per_wave, heads) + row_of_wave; h += rows) {   // the same number of turns for all lanes
-      const bool live = h < min(h0 + a.per_wave, heads);
-      const bool is_q = h < a.heads[0], is_v = h >= a.heads[0] + a.heads[1];
-      const unsigned head = is_q ? h : is_v ? h - a.heads[0] - a.heads[1] : h - a.heads[0];
-      const Rows from = either(is_q, a.q, either(is_v, a.v, a.k));
+    const bool stored = !a.slots || (unsigned long long)slot < a.places;
+    const unsigned page = a.slots && stored ? (unsigned)slot / a.page : 0u, place = a.slots && stored ? (unsigned)slot - page * a.page : 0u;
+    for (unsigned h0 = first; h0 < end; h0 += rows) {
+      const Turn n(a, h0 + row_of_wave, end);
+      const auto now = next;
+      next = load(Turn(a, h0 + rows + row_of_wave, end), t);
       float x[2][V];
-      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(from.ptr) + t * from.token + head * from.head, p, live, x);
+      unpack(now, p, x);
       const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
-      if (!is_v) {
-        const float r = (is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? 1.0f / sqrtf(square * by_dim + a.eps) : 1.0f;
+      if (!n.is_v) {
+        float w[2][V];
+        unpack(either(n.is_q, wq, wk), p, w);
+        const float r = (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? 1.0f / sqrtf(square * by_dim + a.eps) : 1.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float y0 = x[0][i] * r * either(is_q, wq[0][i], wk[0][i]), y1 = x[1][i] * r * either(is_q, wq[1][i], wk[1][i]);
+          const float y0 = x[0][i] * r * w[0][i], y1 = x[1][i] * r * w[1][i];
           x[0][i] = p.turned ? y0 * c[i] - y1 * s[i] : y0;
           x[1][i] = p.turned ? y1 * c[i] + y0 * s[i] : y1;
         }
       }
-      if (!live || (!is_q && !stored)) continue;
+      if (!n.live || (!n.is_q && !stored)) continue;
       T *to;
-      if (is_q) to = reinterpret_cast<T *>(a.q_out.ptr) + t * a.q_out.token + head * a.q_out.head;
-      else if (is_v) to = reinterpret_cast<T *>(a.v_cache) + page * a.v_page + place * a.v_place + head * a.v_head;
-      else if (a.slots) to = reinterpret_cast<T *>(a.k_out.ptr) + page * a.k_page + place * a.k_place + head * a.k_out.head;
-      else to = reinterpret_cast<T *>(a.k_out.ptr) + t * a.k_out.token + head * a.k_out.head;
-      store_row<T, V, Interleaved>(to, p, x);
+      if (n.is_q) to = row_of<T>(a.q_out, t, n.head);
+      else if (n.is_v) to = reinterpret_cast<T *>(a.v_cache) + page * a.v_page + place * a.v_place + n.head * a.v_head;
+      else if (a.slots) to = reinterpret_cast<T *>(a.k_out.ptr) + page * a.k_page + place * a.k_place + n.head * a.k_out.head;
+      else to = row_of<T>(a.k_out, t, n.head);
+      store_row<Stream>(to, p, x);
     }
   }
 }
@@ -217,64 +242,60 @@ struct GradRows {
 };
 
 // dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
-
-template <class T, int V, bool Interleaved>
+template <class T, int V, bool Interleaved, bool Stream>
 __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
-  __shared__ float sums[kWaves][2][kMostDim];
+  __shared__ alignas(32) float sums[kWaves][2][kMostDim];
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
   const Place<V, Interleaved> p(a.dim, a.half, chunk);
-  float wq[2][V], wk[2][V], dq[2][V], dk[2][V];
-  load_weight<T, V, Interleaved>(a, 0, p, wq);
-  load_weight<T, V, Interleaved>(a, 1, p, wk);
+  const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
+  float dq[2][V], dk[2][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) dq[0][i] = dq[1][i] = dk[0][i] = dk[1][i] = 0.0f;
-  const unsigned heads = a.heads[0] + a.heads[1], parts = (heads + a.per_wave - 1) / a.per_wave;
-  const unsigned long long units = (unsigned long long)a.tokens * parts;
+  const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1]);
   const float by_dim = 1.0f / (float)a.dim;
-  for (unsigned long long u = (unsigned long long)blockIdx.x * kWaves + wave_id(); u < units; u += (unsigned long long)gridDim.x * kWaves) {
-    const unsigned t = (unsigned)(u / parts), h0 = (unsigned)(u % parts) * a.per_wave;
+  auto load_x = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, a.k), t, n.head), p, n.live); };
+  auto load_g = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, rows_of.dy[0], rows_of.dy[1]), t, n.head), p, n.live); };
+  for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
+    auto next_x = load_x(Turn(a, first + row_of_wave, end), t), next_g = load_g(Turn(a, first + row_of_wave, end), t);
     float c[V], s[V];
     load_angles(a, p, t, c, s);
-    for (unsigned h = h0 + row_of_wave; h < min(h0 + a.per_wave, heads) + row_of_wave; h += rows) {   // the same number of turns for all lanes
-      const bool live = h < min(h0 + a.per_wave, heads);
-      const bool is_q = h < a.heads[0];
-      const unsigned head = is_q ? h : h - a.heads[0];
-      const Rows from = either(is_q, a.q, a.k), up = either(is_q, rows_of.dy[0], rows_of.dy[1]);
+    for (unsigned h0 = first; h0 < end; h0 += rows) {
+      const Turn n(a, h0 + row_of_wave, end);
       float x[2][V], g[2][V];
-      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(from.ptr) + t * from.token + head * from.head, p, live, x);
-      load_row<T, V, Interleaved>(reinterpret_cast<const T *>(up.ptr) + t * up.token + head * up.head, p, live, g);
+      unpack(next_x, p, x);
+      unpack(next_g, p, g);
+      const Turn then(a, h0 + rows + row_of_wave, end);
+      next_x = load_x(then, t);
+      next_g = load_g(then, t);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float g0 = g[0][i], g1 = g[1][i];
-        if (p.turned) {
-          g[0][i] = g0 * c[i] + g1 * s[i];
-          g[1][i] = g1 * c[i] - g0 * s[i];
-        }
+        g[0][i] = p.turned ? g0 * c[i] + g1 * s[i] : g0;
+        g[1][i] = p.turned ? g1 * c[i] - g0 * s[i] : g1;
       }
-      if (is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
+      if (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
         // the sums are taken by all lanes of a row together: a row is of q or of k as a whole
         const float r = 1.0f / sqrtf(lanes_sum(sum_of_products(x, x), (int)a.lanes_log2) * by_dim + a.eps);
-        float gw[2][V];
+        float w[2][V];
+        unpack(either(n.is_q, wq, wk), p, w);
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             x[k][i] *= r;
-            const float dw = live ? g[k][i] * x[k][i] : 0.0f;
-            dq[k][i] += is_q ? dw : 0.0f;
-            dk[k][i] += is_q ? 0.0f : dw;
-            gw[k][i] = g[k][i] * either(is_q, wq[k][i], wk[k][i]);
+            const float dw = g[k][i] * x[k][i];              // zero where the row is not live
+            dq[k][i] += n.is_q ? dw : 0.0f;
+            dk[k][i] += n.is_q ? 0.0f : dw;
+            g[k][i] *= w[k][i];
           }
-        const float mean = lanes_sum(sum_of_products(gw, x), (int)a.lanes_log2) * by_dim;
+        const float mean = lanes_sum(sum_of_products(g, x), (int)a.lanes_log2) * by_dim;
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) g[k][i] = r * (gw[k][i] - x[k][i] * mean);
+          for (int k = 0; k < 2; ++k) g[k][i] = r * (g[k][i] - x[k][i] * mean);
       }
-      if (!live) continue;
-      const Rows to = either(is_q, rows_of.dx[0], rows_of.dx[1]);
-      store_row<T, V, Interleaved>(reinterpret_cast<T *>(to.ptr) + t * to.token + head * to.head, p, g);
+      if (n.live) store_row<Stream>(row_of<T>(either(n.is_q, rows_of.dx[0], rows_of.dx[1]), t, n.head), p, g);
     }
   }
   if (!partial) return;
@@ -288,46 +309,59 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradR
         dk[k][i] += __shfl_xor(dk[k][i], (int)d);
       }
   if (row_of_wave == 0) {
-    store_row<float, V, Interleaved>(sums[wave_id()][0], p, dq);
-    store_row<float, V, Interleaved>(sums[wave_id()][1], p, dk);
+    store_row<false>(sums[wave_id()][0], p, dq);
+    store_row<false>(sums[wave_id()][1], p, dk);
   }
   __syncthreads();
+  const unsigned group = blockIdx.y * gridDim.x + blockIdx.x;
   for (unsigned i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
     const unsigned which = i >= a.dim, d = i - which * a.dim;
     float sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += sums[w][which][d];
-    partial[(unsigned long long)blockIdx.x * 2 * a.dim + i] = sum;
+    partial[(unsigned long long)group * 2 * a.dim + i] = sum;
   }
 }
 
-// dw[i] = sum of partial[g][i] over the groups: 16 columns a workgroup, 16 threads a column
-__global__ __launch_bounds__(kThreads) void weight_grad_kernel(const float *partial, unsigned groups, unsigned dim, float *dq, float *dk) {
-  __shared__ float sums[16][17];
-  const unsigned column = blockIdx.x * 16 + (threadIdx.x & 15), of = threadIdx.x >> 4;
+// dw[i] = sum of partial[g][i] over the groups: kColumns columns a workgroup, the groups shared by its threads, eight of a thread's on
+// their way at a time
+constexpr int kColumns = 8, kAdders = 1024 / kColumns;
+__global__ __launch_bounds__(1024) void weight_grad_kernel(const float *partial, unsigned groups, unsigned dim, float *dq, float *dk) {
+  __shared__ float sums[kAdders][kColumns + 1];
+  const unsigned mine = threadIdx.x % kColumns, column = blockIdx.x * kColumns + mine, of = threadIdx.x / kColumns;
   float sum = 0.0f;
   if (column < 2 * dim)
-    for (unsigned g = of; g < groups; g += 16) sum += partial[(unsigned long long)g * 2 * dim + column];
-  sums[of][threadIdx.x & 15] = sum;
+    for (unsigned g = of; g < groups; g += 8 * kAdders) {
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = g + k * kAdders < groups ? partial[(unsigned long long)(g + k * kAdders) * 2 * dim + column] : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += x[k];
+    }
+  sums[of][mine] = sum;
   __syncthreads();
-  if (of != 0 || column >= 2 * dim) return;
+  // the first wave: 8 threads a column, each 16 of the sums, then the 8
+  if (threadIdx.x >= 8 * kColumns) return;
   sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) sum += sums[k][threadIdx.x];
+  for (int k = 0; k < kAdders / 8; ++k) sum += sums[k * 8 + of][mine];
+#pragma unroll
+  for (int d = kColumns; d < 8 * kColumns; d *= 2) sum += __shfl_xor(sum, d);
   float *to = column < dim ? dq : dk;
-  if (to) to[column < dim ? column : column - dim] = sum;
+  if (of == 0 && column < 2 * dim && to) to[column < dim ? column : column - dim] = sum;
 }
 
 // ------------------------------------------------------------------ host
-// calls f with the type, the elements of a pack and the pairing of this call as compile-time values
-template <class F> void with_form(int32_t dtype, int pack, bool interleaved, F &&f) {
+// calls f with the type, the elements of a pack, the pairing and the way through the caches of this call as compile-time values
+template <class F> void with_form(int32_t dtype, int pack, bool interleaved, bool stream, F &&f) {
   auto by_pack = [&](auto element, auto paired) {
     using T = decltype(element);
-    if constexpr (sizeof(T) == 2)
-      if (pack == 8) { f(element, std::integral_constant<int, 8>{}, paired); return; }
-    if (pack == 4) f(element, std::integral_constant<int, 4>{}, paired);
-    else if (pack == 2) f(element, std::integral_constant<int, 2>{}, paired);
-    else f(element, std::integral_constant<int, 1>{}, paired);
+    constexpr int kWide = 16 / sizeof(T);
+    if (pack == kWide && stream) f(element, std::integral_constant<int, kWide>{}, paired, std::true_type{});
+    else if (pack == kWide) f(element, std::integral_constant<int, kWide>{}, paired, std::false_type{});
+    else if (kWide > 4 && pack == 4) f(element, std::integral_constant<int, 4>{}, paired, std::false_type{});
+    else if (pack == 2) f(element, std::integral_constant<int, 2>{}, paired, std::false_type{});
+    else f(element, std::integral_constant<int, 1>{}, paired, std::false_type{});
   };
   auto by_pairing = [&](auto element) { interleaved ? by_pack(element, std::true_type{}) : by_pack(element, std::false_type{}); };
   if (dtype == FC_F32) by_pairing(float{});
@@ -342,14 +376,18 @@ struct HeadsCall {
   int32_t dtype;
   int pack;
   bool interleaved;
-  // how the heads of a token are shared among waves, and the workgroups that are then needed, `most` at most
-  unsigned shape(unsigned heads, unsigned most) {
-    const unsigned rows = kWave >> a.lanes_log2;
-    // a wave takes all heads of a token, unless that leaves compute units without work
-    const unsigned turns = ceil_div(heads, rows);
-    const unsigned parts = std::min<unsigned>(turns, std::max(1u, 4096u / std::max(1u, a.tokens)));
+  bool stream = false;
+  dim3 grid;
+  // How the heads of a token are shared among waves (grid.y), and the workgroups that are then needed, `most` at most.  A wave takes all
+  // heads of a token, unless that leaves compute units without work.
+  void shape(unsigned heads, unsigned most) {
+    const unsigned rows = kWave >> a.lanes_log2, turns = std::max(1u, ceil_div(heads, rows));
+    const unsigned parts = std::min({turns, std::max(1u, 4096u / std::max(1u, a.tokens)), most});
     a.per_wave = ceil_div(turns, parts) * rows;
-    return std::min(std::max(ceil_div((unsigned long long)a.tokens * ceil_div(heads, a.per_wave), kWaves), 1u), most);
+    grid.y = std::max(1u, ceil_div(heads, a.per_wave));
+    grid.x = std::max(1u, std::min(ceil_div(a.tokens, kWaves), most / grid.y));
+    // what is read and written passes the caches where they would not hold it until it is used
+    stream = (unsigned long long)a.tokens * heads * a.dim * (dtype == FC_F32 ? 4 : 2) >= 32u << 20;
   }
 };
 
@@ -418,11 +456,10 @@ int settle_lanes(TensorChecks &c, HeadsCall &call) {
 }
 
 struct HeadNormRope final : Operator, HeadsCall {
-  unsigned grid = 0;
   void record(Recorder &r) const override {
     if (a.tokens == 0 || a.heads[0] + a.heads[1] + a.heads[2] == 0) return;
-    with_form(dtype, pack, interleaved, [&](auto element, auto v, auto paired) {
-      r.launch(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value>, grid, kThreads, a);
+    with_form(dtype, pack, interleaved, stream, [&](auto element, auto v, auto paired, auto past) {
+      r.launch(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>, grid, kThreads, a);
     });
   }
   const char *name() const override { return "head norm and rotation"; }
@@ -431,15 +468,15 @@ struct HeadNormRope final : Operator, HeadsCall {
 struct HeadNormRopeGrad final : Operator, HeadsCall {
   GradRows rows{};
   float *dw[2] = {nullptr, nullptr};
-  unsigned grid = 0;
-  size_t workspace() const override { return dw[0] || dw[1] ? (size_t)grid * 2 * a.dim * sizeof(float) : 0; }
+  unsigned groups() const { return grid.x * grid.y; }
+  size_t workspace() const override { return dw[0] || dw[1] ? (size_t)groups() * 2 * a.dim * sizeof(float) : 0; }
   void record(Recorder &r) const override {
     float *partial = dw[0] || dw[1] ? reinterpret_cast<float *>(r.workspace) : nullptr;
     if (!partial && (a.tokens == 0 || a.heads[0] + a.heads[1] == 0)) return;
-    with_form(dtype, pack, interleaved, [&](auto element, auto v, auto paired) {
-      r.launch(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value>, grid, kThreads, a, rows, partial);
+    with_form(dtype, pack, interleaved, stream, [&](auto element, auto v, auto paired, auto past) {
+      r.launch(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>, grid, kThreads, a, rows, partial);
     });
-    if (partial) r.launch(&weight_grad_kernel, ceil_div(2 * a.dim, 16), kThreads, (const float *)partial, grid, a.dim, dw[0], dw[1]);
+    if (partial) r.launch(&weight_grad_kernel, ceil_div(2 * a.dim, kColumns), 1024, (const float *)partial, groups(), a.dim, dw[0], dw[1]);
   }
   const char *name() const override { return "gradient of head norm and rotation"; }
 };
@@ -466,8 +503,9 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
     a.slots = static_cast<const long long *>(n.slots.ptr);
     a.heads[2] = (unsigned)kv;
     a.v = rows_at(n.v);
-    a.pages = (unsigned)n.k_cache.shape[0];
+    if (n.k_cache.shape[0] * n.k_cache.shape[1] > 0x7fffffff) return c.fail(FC_E_LIMIT, "k_cache: more than 2^31-1 places").code();
     a.page = (unsigned)n.k_cache.shape[1];
+    a.places = (unsigned)(n.k_cache.shape[0] * n.k_cache.shape[1]);
     a.k_out = {static_cast<char *>(n.k_cache.ptr), 0, n.k_cache.stride[2]};
     a.v_cache = static_cast<char *>(n.v_cache.ptr);
     a.k_page = n.k_cache.stride[0];
@@ -485,7 +523,7 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
   if (!c.ok()) return c.code();
   align(n.q_out);
   if (settle_lanes(c, *op) != FC_OK) return c.code();
-  op->grid = op->shape(a.heads[0] + a.heads[1] + a.heads[2], 4096);
+  op->shape(a.heads[0] + a.heads[1] + a.heads[2], 4096);
   out = std::move(op);
   return FC_OK;
 }
@@ -510,7 +548,7 @@ int make_head_norm_rope_grad(const fc_head_norm_rope_grad &n, std::unique_ptr<Op
   if (settle_lanes(c, *op) != FC_OK) return c.code();
   op->dw[0] = present(n.dq_weight) ? static_cast<float *>(n.dq_weight.ptr) : nullptr;
   op->dw[1] = present(n.dk_weight) ? static_cast<float *>(n.dk_weight.ptr) : nullptr;
-  op->grid = op->shape(a.heads[0] + a.heads[1], kGradGroups);
+  op->shape(a.heads[0] + a.heads[1], kGradGroups);
   out = std::move(op);
   return FC_OK;
 }

@@ -25,8 +25,8 @@ struct Recorder {
   unsigned *counters;              // DEVICE: kCounters of them, 0 between launches
   const char *what;                // the operator, for the message of a launch that fails
 
-  template <class... P, class... A> void launch(void (*kernel)(P...), unsigned grid, unsigned threads, const A &...a) {
-    keep(kernel, dim3(grid), dim3(threads), std::make_shared<std::tuple<P...>>(a...), std::index_sequence_for<P...>());
+  template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, unsigned threads, const A &...a) {
+    keep(kernel, grid, dim3(threads), std::make_shared<std::tuple<P...>>(a...), std::index_sequence_for<P...>());
   }
 
  private:
@@ -96,8 +96,15 @@ template <> struct ElementOf<FC_BF16> { using T = __bf16; };
 
 template <class T, int N> using Vec = T __attribute__((ext_vector_type(N)));      // aligned to its size
 
-template <class T, int N> __device__ __forceinline__ Vec<T, N> load_vec(const T *p) { return *reinterpret_cast<const Vec<T, N> *>(p); }
-template <class T, int N> __device__ __forceinline__ void store_vec(T *p, Vec<T, N> v) { *reinterpret_cast<Vec<T, N> *>(p) = v; }
+// Stream: past the caches, for what is used once (16 bytes)
+template <class T, int N, bool Stream = false> __device__ __forceinline__ Vec<T, N> load_vec(const T *p) {
+  if constexpr (Stream) return __builtin_bit_cast(Vec<T, N>, __builtin_nontemporal_load(reinterpret_cast<const Vec<unsigned, 4> *>(p)));
+  else return *reinterpret_cast<const Vec<T, N> *>(p);
+}
+template <class T, int N, bool Stream = false> __device__ __forceinline__ void store_vec(T *p, Vec<T, N> v) {
+  if constexpr (Stream) __builtin_nontemporal_store(__builtin_bit_cast(Vec<unsigned, 4>, v), reinterpret_cast<Vec<unsigned, 4> *>(p));
+  else *reinterpret_cast<Vec<T, N> *>(p) = v;
+}
 
 // Sum over groups of 2^log2 neighbouring lanes, every lane gets it.  Up to 16 lanes by DPP: after the steps within four lanes, the
 // mirror of eight and of sixteen bring the other half's sum.
