@@ -41,10 +41,17 @@ struct HeadsArgs {
 // Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.
 template <int V, bool Interleaved> struct Place {
   unsigned at[2], pair;             // pair: of the first elements
+  unsigned axes[(V + 3) / 4];       // of the pairs, a byte each; 255: none
   bool any, turned;
-  __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
+  __device__ __forceinline__ unsigned axis_of(int i) const { return axes[i / 4] >> (8 * (i % 4)) & 255u; }
+  __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk, const int *axis_of) {
     any = 2 * V * chunk < dim;
     turned = V * chunk < half;
+#pragma unroll
+    for (int k = 0; k < (V + 3) / 4; ++k) axes[k] = 0;
+    if (axis_of && turned)
+#pragma unroll
+      for (int i = 0; i < V; ++i) axes[i / 4] |= (unsigned)min((unsigned)axis_of[V * chunk + i], 255u) << (8 * (i % 4));
     pair = V * chunk;
     at[0] = turned && !Interleaved ? V * chunk : 2 * V * chunk;
     at[1] = turned && !Interleaved ? half + V * chunk : 2 * V * chunk + V;
@@ -103,48 +110,40 @@ __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p
   store_vec<T, V, Stream>(row + p.at[1], b);
 }
 
-// Cosines and sines of the pairs of this lane at token t: 1 and 0 where nothing is turned, NaN where the table has no row.
+// Cosines and sines of the pairs of this lane at token t: 1 and 0 where nothing is turned, NaN where the tables have no row.  The pairs of a
+// lane lie side by side, so a row of each axis is read whole and the pairs take theirs.
 template <int V, bool Interleaved>
 __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
+  constexpr int N = V < 4 ? V : 4;
   const bool on = a.cos_sin && p.any && p.turned;
-  if (!a.axis_of) {                 // one position a token: the lane's pairs lie side by side
-    constexpr int N = V < 4 ? V : 4;
-    const int at = on && a.axes ? a.positions[t] : -1;
-    const bool there = (unsigned)at < a.angles;
-    const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + p.pair;
-#pragma unroll
-    for (int i = 0; i < V; i += N) {
-      const float missing = on ? __builtin_nanf("") : 1.0f;
-      Vec<float, N> cosine, sine;
-#pragma unroll
-      for (int k = 0; k < N; ++k) { cosine[k] = missing; sine[k] = missing - 1.0f; }
-      if (there) {
-        if (a.wide_angles) {
-          cosine = load_vec<float, N>(row + i);
-          sine = load_vec<float, N>(row + a.half + i);
-        } else {
-#pragma unroll
-          for (int k = 0; k < N; ++k) { cosine[k] = row[i + k]; sine[k] = row[a.half + i + k]; }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < N; ++k) { c[i + k] = cosine[k]; s[i + k] = sine[k]; }
-    }
-    return;
-  }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    float cosine = 1.0f, sine = 0.0f;
-    if (on) {
-      const int axis = a.axis_of[p.pair + i];
-      const int at = (unsigned)axis < a.axes ? a.positions[axis * a.position_stride + t] : -1;
-      const bool there = (unsigned)at < a.angles;
-      const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + p.pair + i;
-      cosine = there ? row[0] : __builtin_nanf("");
-      sine = there ? row[a.half] : __builtin_nanf("");
+    c[i] = on ? __builtin_nanf("") : 1.0f;
+    s[i] = on ? __builtin_nanf("") : 0.0f;
+  }
+  if (!a.cos_sin) return;
+  const unsigned axes = a.axis_of ? a.axes : min(a.axes, 1u);
+  for (unsigned axis = 0; axis < axes; ++axis) {
+    const int at = load_scalar(a.positions + axis * a.position_stride + t);
+    if ((unsigned)at >= a.angles) continue;
+    const float *row = a.cos_sin + at * a.angle_stride + (on ? p.pair : 0u);
+#pragma unroll
+    for (int i = 0; i < V; i += N) {
+      Vec<float, N> cosine, sine;
+      if (a.wide_angles) {
+        cosine = load_vec<float, N>(row + i);
+        sine = load_vec<float, N>(row + a.half + i);
+      } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) { cosine[k] = row[i + k]; sine[k] = row[a.half + i + k]; }
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const bool mine = on && p.axis_of(i + k) == axis;
+        c[i + k] = mine ? cosine[k] : c[i + k];
+        s[i + k] = mine ? sine[k] : s[i + k];
+      }
     }
-    c[i] = cosine;
-    s[i] = sine;
   }
 }
 
@@ -193,7 +192,7 @@ template <class T, int V, bool Interleaved, bool Stream>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk);
+  const Place<V, Interleaved> p(a.dim, a.half, chunk, a.axis_of);
   const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
   const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1] + a.heads[2]);
   const float by_dim = 1.0f / (float)a.dim;
@@ -202,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
     auto next = load(Turn(a, first + row_of_wave, end), t);
     float c[V], s[V];
     load_angles(a, p, t, c, s);
-    const long long slot = a.slots ? a.slots[t] : 0;
+    const long long slot = a.slots ? load_scalar(a.slots + t) : 0;
     const bool stored = !a.slots || (unsigned long long)slot < a.places;
     const unsigned page = a.slots && stored ? (unsigned)slot / a.page : 0u, place = a.slots && stored ? (unsigned)slot - page * a.page : 0u;
     for (unsigned h0 = first; h0 < end; h0 += rows) {
@@ -235,7 +234,6 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
 }
 
 constexpr unsigned kMostDim = 512;
-constexpr unsigned kGradGroups = 1024;      // workgroups of the gradient at most: one row of partial sums for each
 
 struct GradRows {
   Rows dy[2], dx[2];                        // of q and of k
@@ -247,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradR
   __shared__ alignas(32) float sums[kWaves][2][kMostDim];
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk);
+  const Place<V, Interleaved> p(a.dim, a.half, chunk, a.axis_of);
   const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
   float dq[2][V], dk[2][V];
 #pragma unroll
@@ -376,18 +374,21 @@ struct HeadsCall {
   int32_t dtype;
   int pack;
   bool interleaved;
-  bool stream = false;
   dim3 grid;
-  // How the heads of a token are shared among waves (grid.y), and the workgroups that are then needed, `most` at most.  A wave takes all
-  // heads of a token, unless that leaves compute units without work.
-  void shape(unsigned heads, unsigned most) {
-    const unsigned rows = kWave >> a.lanes_log2, turns = std::max(1u, ceil_div(heads, rows));
+  unsigned heads() const { return a.heads[0] + a.heads[1] + a.heads[2]; }
+  // What is read and written passes the caches where they would not hold it until it is used (16384 tokens of 40 heads 70 us through them,
+  // 63 past them).
+  bool stream() const { return (unsigned long long)a.tokens * heads() * a.dim * size_of_dtype(dtype) >= 32u << 20; }
+  // How the heads of a token are shared among waves (grid.y), and the workgroups that are then needed, as many as are resident at once at
+  // most: a second round of a few lasts as long as the first (the gradient of 16384 tokens on 768 workgroups 95 us, 1024 117).  A wave takes
+  // all heads of a token, unless that leaves compute units without work.
+  template <class... P> void shape(void (*kernel)(P...)) {
+    const unsigned resident = resident_workgroups(kernel, kThreads), most = resident ? resident : 768u;
+    const unsigned rows = kWave >> a.lanes_log2, turns = std::max(1u, ceil_div(heads(), rows));
     const unsigned parts = std::min({turns, std::max(1u, 4096u / std::max(1u, a.tokens)), most});
     a.per_wave = ceil_div(turns, parts) * rows;
-    grid.y = std::max(1u, ceil_div(heads, a.per_wave));
+    grid.y = std::max(1u, ceil_div(heads(), a.per_wave));
     grid.x = std::max(1u, std::min(ceil_div(a.tokens, kWaves), most / grid.y));
-    // what is read and written passes the caches where they would not hold it until it is used
-    stream = (unsigned long long)a.tokens * heads * a.dim * (dtype == FC_F32 ? 4 : 2) >= 32u << 20;
   }
 };
 
@@ -407,6 +408,7 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
     c.array("positions", positions, FC_I32, {-1, tokens});
     if (c.ok() && (cos_sin.shape[1] % 2 || cos_sin.shape[1] > dim)) c.fail(FC_E_ARG, "cos_sin: an even number of columns, at most the elements of a head, is needed");
     if (present(axis_of)) c.array("axis_of", axis_of, FC_I32, {cos_sin.shape[1] / 2});
+    if (c.ok() && positions.shape[0] > 255) c.fail(FC_E_LIMIT, "positions: more than 255 axes");
   } else if (present(positions) || present(axis_of)) {
     c.fail(FC_E_ARG, "positions and axis_of go with cos_sin");
   }
@@ -456,11 +458,14 @@ int settle_lanes(TensorChecks &c, HeadsCall &call) {
 }
 
 struct HeadNormRope final : Operator, HeadsCall {
-  void record(Recorder &r) const override {
-    if (a.tokens == 0 || a.heads[0] + a.heads[1] + a.heads[2] == 0) return;
-    with_form(dtype, pack, interleaved, stream, [&](auto element, auto v, auto paired, auto past) {
-      r.launch(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>, grid, kThreads, a);
+  template <class F> void with_kernel(F &&f) const {
+    with_form(dtype, pack, interleaved, stream(), [&](auto element, auto v, auto paired, auto past) {
+      f(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>);
     });
+  }
+  void record(Recorder &r) const override {
+    if (a.tokens == 0 || heads() == 0) return;
+    with_kernel([&](auto kernel) { r.launch(kernel, grid, kThreads, a); });
   }
   const char *name() const override { return "head norm and rotation"; }
 };
@@ -470,12 +475,15 @@ struct HeadNormRopeGrad final : Operator, HeadsCall {
   float *dw[2] = {nullptr, nullptr};
   unsigned groups() const { return grid.x * grid.y; }
   size_t workspace() const override { return dw[0] || dw[1] ? (size_t)groups() * 2 * a.dim * sizeof(float) : 0; }
+  template <class F> void with_kernel(F &&f) const {
+    with_form(dtype, pack, interleaved, stream(), [&](auto element, auto v, auto paired, auto past) {
+      f(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>);
+    });
+  }
   void record(Recorder &r) const override {
     float *partial = dw[0] || dw[1] ? reinterpret_cast<float *>(r.workspace) : nullptr;
-    if (!partial && (a.tokens == 0 || a.heads[0] + a.heads[1] == 0)) return;
-    with_form(dtype, pack, interleaved, stream, [&](auto element, auto v, auto paired, auto past) {
-      r.launch(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>, grid, kThreads, a, rows, partial);
-    });
+    if (!partial && (a.tokens == 0 || heads() == 0)) return;
+    with_kernel([&](auto kernel) { r.launch(kernel, grid, kThreads, a, rows, partial); });
     if (partial) r.launch(&weight_grad_kernel, ceil_div(2 * a.dim, kColumns), 1024, (const float *)partial, groups(), a.dim, dw[0], dw[1]);
   }
   const char *name() const override { return "gradient of head norm and rotation"; }
@@ -523,7 +531,7 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
   if (!c.ok()) return c.code();
   align(n.q_out);
   if (settle_lanes(c, *op) != FC_OK) return c.code();
-  op->shape(a.heads[0] + a.heads[1] + a.heads[2], 4096);
+  op->with_kernel([&](auto kernel) { op->shape(kernel); });
   out = std::move(op);
   return FC_OK;
 }
@@ -548,7 +556,7 @@ int make_head_norm_rope_grad(const fc_head_norm_rope_grad &n, std::unique_ptr<Op
   if (settle_lanes(c, *op) != FC_OK) return c.code();
   op->dw[0] = present(n.dq_weight) ? static_cast<float *>(n.dq_weight.ptr) : nullptr;
   op->dw[1] = present(n.dk_weight) ? static_cast<float *>(n.dk_weight.ptr) : nullptr;
-  op->shape(a.heads[0] + a.heads[1], kGradGroups);
+  op->with_kernel([&](auto kernel) { op->shape(kernel); });
   out = std::move(op);
   return FC_OK;
 }

@@ -106,6 +106,11 @@ template <class T, int N, bool Stream = false> __device__ __forceinline__ void s
   else *reinterpret_cast<Vec<T, N> *>(p) = v;
 }
 
+// an element that this kernel does not write, for the whole wave: through the scalar unit, which has a counter of its own to wait for
+template <class T> __device__ __forceinline__ T load_scalar(const T *p) {
+  return *reinterpret_cast<const T __attribute__((address_space(4))) *>(reinterpret_cast<uintptr_t>(p));
+}
+
 // Sum over groups of 2^log2 neighbouring lanes, every lane gets it.  Up to 16 lanes by DPP: after the steps within four lanes, the
 // mirror of eight and of sixteen bring the other half's sum.
 __device__ __forceinline__ float lanes_sum(float v, int log2) {

@@ -86,11 +86,6 @@ template <class F> __device__ __forceinline__ float over_column(float v, F &&f) 
 __device__ __forceinline__ float column_max(float v) { return over_column(v, [](float x, float y) { return fmaxf(x, y); }); }
 __device__ __forceinline__ float column_sum(float v) { return over_column(v, [](float x, float y) { return x + y; }); }
 
-// an element that this kernel does not write, for the whole wave: through the scalar unit, which has a counter of its own to wait for
-template <class T> __device__ __forceinline__ T load_scalar(const T *p) {
-  return *reinterpret_cast<const T __attribute__((address_space(4))) *>(reinterpret_cast<uintptr_t>(p));
-}
-
 // a value that all lanes have, in scalar registers
 __device__ __forceinline__ unsigned uniform(unsigned v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ unsigned long long uniform(unsigned long long v) { return (unsigned long long)uniform((unsigned)(v >> 32)) << 32 | uniform((unsigned)v); }
