@@ -110,39 +110,56 @@ __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p
   store_vec<T, V, Stream>(row + p.at[1], b);
 }
 
-// Cosines and sines of the pairs of this lane at token t: 1 and 0 where nothing is turned, NaN where the tables have no row.  The pairs of a
+// V elements of a row of angles from `row` on
+template <int V> __device__ __forceinline__ void load_floats(const HeadsArgs &a, const float *row, float (&x)[V]) {
+  constexpr int N = V < 4 ? V : 4;
+#pragma unroll
+  for (int i = 0; i < V; i += N) {
+    Vec<float, N> part;
+    if (a.wide_angles) part = load_vec<float, N>(row + i);
+    else
+#pragma unroll
+      for (int k = 0; k < N; ++k) part[k] = row[i + k];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[i + k] = part[k];
+  }
+}
+
+// Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  The pairs of a
 // lane lie side by side, so a row of each axis is read whole and the pairs take theirs.
 template <int V, bool Interleaved>
 __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
-  constexpr int N = V < 4 ? V : 4;
-  const bool on = a.cos_sin && p.any && p.turned;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    c[i] = on ? __builtin_nanf("") : 1.0f;
-    s[i] = on ? __builtin_nanf("") : 0.0f;
-  }
   if (!a.cos_sin) return;
-  const unsigned axes = a.axis_of ? a.axes : min(a.axes, 1u);
-  for (unsigned axis = 0; axis < axes; ++axis) {
+  const unsigned at_lane = p.any && p.turned ? p.pair : 0u;
+  if (!a.axis_of) {
+    const int at = a.axes ? load_scalar(a.positions + t) : -1;
+    const bool there = (unsigned)at < a.angles;
+    const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + at_lane;
+    if (a.angles) {
+      load_floats(a, row, c);
+      load_floats(a, row + a.half, s);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      c[i] = there ? c[i] : __builtin_nanf("");
+      s[i] = there ? s[i] : __builtin_nanf("");
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
+  for (unsigned axis = 0; axis < a.axes; ++axis) {
     const int at = load_scalar(a.positions + axis * a.position_stride + t);
     if ((unsigned)at >= a.angles) continue;
-    const float *row = a.cos_sin + at * a.angle_stride + (on ? p.pair : 0u);
+    const float *row = a.cos_sin + at * a.angle_stride + at_lane;
+    float cosine[V], sine[V];
+    load_floats(a, row, cosine);
+    load_floats(a, row + a.half, sine);
 #pragma unroll
-    for (int i = 0; i < V; i += N) {
-      Vec<float, N> cosine, sine;
-      if (a.wide_angles) {
-        cosine = load_vec<float, N>(row + i);
-        sine = load_vec<float, N>(row + a.half + i);
-      } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) { cosine[k] = row[i + k]; sine[k] = row[a.half + i + k]; }
-      }
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const bool mine = on && p.axis_of(i + k) == axis;
-        c[i + k] = mine ? cosine[k] : c[i + k];
-        s[i + k] = mine ? sine[k] : s[i + k];
-      }
+    for (int i = 0; i < V; ++i) {
+      const bool mine = p.axis_of(i) == axis;
+      c[i] = mine ? cosine[i] : c[i];
+      s[i] = mine ? sine[i] : s[i];
     }
   }
 }
@@ -199,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   auto load = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, either(n.is_v, a.v, a.k)), t, n.head), p, n.live); };
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next = load(Turn(a, first + row_of_wave, end), t);
-    float c[V], s[V];
+    float c[V] = {}, s[V] = {};
     load_angles(a, p, t, c, s);
     const long long slot = a.slots ? load_scalar(a.slots + t) : 0;
     const bool stored = !a.slots || (unsigned long long)slot < a.places;
@@ -241,7 +258,7 @@ struct GradRows {
 
 // dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
 template <class T, int V, bool Interleaved, bool Stream>
-__global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
+__global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
   __shared__ alignas(32) float sums[kWaves][2][kMostDim];
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
@@ -256,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadsArgs a, GradR
   auto load_g = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, rows_of.dy[0], rows_of.dy[1]), t, n.head), p, n.live); };
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next_x = load_x(Turn(a, first + row_of_wave, end), t), next_g = load_g(Turn(a, first + row_of_wave, end), t);
-    float c[V], s[V];
+    float c[V] = {}, s[V] = {};
     load_angles(a, p, t, c, s);
     for (unsigned h0 = first; h0 < end; h0 += rows) {
       const Turn n(a, h0 + row_of_wave, end);
