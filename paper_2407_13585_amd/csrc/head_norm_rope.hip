@@ -15,6 +15,7 @@ namespace fc {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr unsigned kMostDim = 512;
 
 struct Rows {                       // [T, heads, D]
   char *ptr;
@@ -41,17 +42,10 @@ struct HeadsArgs {
 // Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.
 template <int V, bool Interleaved> struct Place {
   unsigned at[2], pair;             // pair: of the first elements
-  unsigned axes[(V + 3) / 4];       // of the pairs, a byte each; 255: none
   bool any, turned;
-  __device__ __forceinline__ unsigned axis_of(int i) const { return axes[i / 4] >> (8 * (i % 4)) & 255u; }
-  __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk, const int *axis_of) {
+  __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
     any = 2 * V * chunk < dim;
     turned = V * chunk < half;
-#pragma unroll
-    for (int k = 0; k < (V + 3) / 4; ++k) axes[k] = 0;
-    if (axis_of && turned)
-#pragma unroll
-      for (int i = 0; i < V; ++i) axes[i / 4] |= (unsigned)min((unsigned)axis_of[V * chunk + i], 255u) << (8 * (i % 4));
     pair = V * chunk;
     at[0] = turned && !Interleaved ? V * chunk : 2 * V * chunk;
     at[1] = turned && !Interleaved ? half + V * chunk : 2 * V * chunk + V;
@@ -125,13 +119,24 @@ template <int V> __device__ __forceinline__ void load_floats(const HeadsArgs &a,
   }
 }
 
-// Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  The pairs of a
-// lane lie side by side, so a row of each axis is read whole and the pairs take theirs.
-template <int V, bool Interleaved>
-__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
+// The axes of the pairs lane, lane + 64, .. of a row, a byte each; 255: none.
+__device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
+  unsigned axes = ~0u;
+#pragma unroll
+  for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k)
+    if (const unsigned n = lane_id() + kWave * k; n < a.half) axes = (axes & ~(255u << 8 * k)) | min((unsigned)a.axis_of[n], 255u) << 8 * k;
+  return axes;
+}
+
+// Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  With
+// one axis a lane reads them from the one row of the token.  With several the lanes of the wave read a pair each and share them through LDS, as
+// every row of the wave needs the same (5003 tokens of 16 heads with three axes: 10.9 us; 14.0 where each lane read its pairs from all rows).
+// shared: kMostDim floats of the wave.
+template <bool Axes, int V, bool Interleaved>
+__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned axes, unsigned t, float *shared, float (&c)[V], float (&s)[V]) {
   if (!a.cos_sin) return;
   const unsigned at_lane = p.any && p.turned ? p.pair : 0u;
-  if (!a.axis_of) {
+  if constexpr (!Axes) {
     const int at = a.axes ? load_scalar(a.positions + t) : -1;
     const bool there = (unsigned)at < a.angles;
     const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + at_lane;
@@ -144,23 +149,33 @@ __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, I
       c[i] = there ? c[i] : __builtin_nanf("");
       s[i] = there ? s[i] : __builtin_nanf("");
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-  for (unsigned axis = 0; axis < a.axes; ++axis) {
-    const int at = load_scalar(a.positions + axis * a.position_stride + t);
-    if ((unsigned)at >= a.angles) continue;
-    const float *row = a.cos_sin + at * a.angle_stride + at_lane;
-    float cosine[V], sine[V];
-    load_floats(a, row, cosine);
-    load_floats(a, row + a.half, sine);
+    for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k) {
+      const unsigned n = lane_id() + kWave * k, axis = axes >> 8 * k & 255u;
+      if (n >= a.half) break;
+      const int at = axis < a.axes ? a.positions[axis * a.position_stride + t] : -1;
+      float cosine = __builtin_nanf(""), sine = cosine;
+      if ((unsigned)at < a.angles) {
+        const float *row = a.cos_sin + at * a.angle_stride + n;
+        cosine = row[0];
+        sine = row[a.half];
+      }
+      shared[n] = cosine;
+      shared[kMostDim / 2 + n] = sine;
+    }
+    // the lanes of a wave go together, and the reads of the token before are done as their values are
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    typedef Vec<float, V> Some;
+    const Some cosines = *reinterpret_cast<const Some *>(shared + at_lane), sines = *reinterpret_cast<const Some *>(shared + kMostDim / 2 + at_lane);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const bool mine = p.axis_of(i) == axis;
-      c[i] = mine ? cosine[i] : c[i];
-      s[i] = mine ? sine[i] : s[i];
+      c[i] = cosines[i];
+      s[i] = sines[i];
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -205,19 +220,21 @@ template <int V> __device__ __forceinline__ float sum_of_products(const float (&
   return s;
 }
 
-template <class T, int V, bool Interleaved, bool Stream>
+template <class T, int V, bool Interleaved, bool Stream, bool Axes>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk, a.axis_of);
+  const Place<V, Interleaved> p(a.dim, a.half, chunk);
   const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
   const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1] + a.heads[2]);
   const float by_dim = 1.0f / (float)a.dim;
+  const unsigned axes = Axes ? axes_of_lane(a) : 0u;
+  __shared__ alignas(32) float shared[Axes ? kWaves : 1][Axes ? kMostDim : 1];
   auto load = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, either(n.is_v, a.v, a.k)), t, n.head), p, n.live); };
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next = load(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    load_angles(a, p, t, c, s);
+    load_angles<Axes>(a, p, axes, t, shared[Axes ? wave_id() : 0], c, s);
     const long long slot = a.slots ? load_scalar(a.slots + t) : 0;
     const bool stored = !a.slots || (unsigned long long)slot < a.places;
     const unsigned page = a.slots && stored ? (unsigned)slot / a.page : 0u, place = a.slots && stored ? (unsigned)slot - page * a.page : 0u;
@@ -250,31 +267,30 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   }
 }
 
-constexpr unsigned kMostDim = 512;
-
 struct GradRows {
   Rows dy[2], dx[2];                        // of q and of k
 };
 
 // dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
-template <class T, int V, bool Interleaved, bool Stream>
+template <class T, int V, bool Interleaved, bool Stream, bool Axes>
 __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
   __shared__ alignas(32) float sums[kWaves][2][kMostDim];
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk, a.axis_of);
+  const Place<V, Interleaved> p(a.dim, a.half, chunk);
   const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
   float dq[2][V], dk[2][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) dq[0][i] = dq[1][i] = dk[0][i] = dk[1][i] = 0.0f;
   const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1]);
   const float by_dim = 1.0f / (float)a.dim;
+  const unsigned axes = Axes ? axes_of_lane(a) : 0u;
   auto load_x = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, a.k), t, n.head), p, n.live); };
   auto load_g = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, rows_of.dy[0], rows_of.dy[1]), t, n.head), p, n.live); };
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next_x = load_x(Turn(a, first + row_of_wave, end), t), next_g = load_g(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    load_angles(a, p, t, c, s);
+    load_angles<Axes>(a, p, axes, t, sums[wave_id()][0], c, s);
     for (unsigned h0 = first; h0 < end; h0 += rows) {
       const Turn n(a, h0 + row_of_wave, end);
       float x[2][V], g[2][V];
@@ -368,15 +384,18 @@ __global__ __launch_bounds__(1024) void weight_grad_kernel(const float *partial,
 
 // ------------------------------------------------------------------ host
 // calls f with the type, the elements of a pack, the pairing and the way through the caches of this call as compile-time values
-template <class F> void with_form(int32_t dtype, int pack, bool interleaved, bool stream, F &&f) {
+template <class F> void with_form(int32_t dtype, int pack, bool interleaved, bool stream, bool axes, F &&f) {
+  auto by_axes = [&](auto element, auto v, auto paired, auto past) {
+    axes ? f(element, v, paired, past, std::true_type{}) : f(element, v, paired, past, std::false_type{});
+  };
   auto by_pack = [&](auto element, auto paired) {
     using T = decltype(element);
     constexpr int kWide = 16 / sizeof(T);
-    if (pack == kWide && stream) f(element, std::integral_constant<int, kWide>{}, paired, std::true_type{});
-    else if (pack == kWide) f(element, std::integral_constant<int, kWide>{}, paired, std::false_type{});
-    else if (kWide > 4 && pack == 4) f(element, std::integral_constant<int, 4>{}, paired, std::false_type{});
-    else if (pack == 2) f(element, std::integral_constant<int, 2>{}, paired, std::false_type{});
-    else f(element, std::integral_constant<int, 1>{}, paired, std::false_type{});
+    if (pack == kWide && stream) by_axes(element, std::integral_constant<int, kWide>{}, paired, std::true_type{});
+    else if (pack == kWide) by_axes(element, std::integral_constant<int, kWide>{}, paired, std::false_type{});
+    else if (kWide > 4 && pack == 4) by_axes(element, std::integral_constant<int, 4>{}, paired, std::false_type{});
+    else if (pack == 2) by_axes(element, std::integral_constant<int, 2>{}, paired, std::false_type{});
+    else by_axes(element, std::integral_constant<int, 1>{}, paired, std::false_type{});
   };
   auto by_pairing = [&](auto element) { interleaved ? by_pack(element, std::true_type{}) : by_pack(element, std::false_type{}); };
   if (dtype == FC_F32) by_pairing(float{});
@@ -476,8 +495,8 @@ int settle_lanes(TensorChecks &c, HeadsCall &call) {
 
 struct HeadNormRope final : Operator, HeadsCall {
   template <class F> void with_kernel(F &&f) const {
-    with_form(dtype, pack, interleaved, stream(), [&](auto element, auto v, auto paired, auto past) {
-      f(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>);
+    with_form(dtype, pack, interleaved, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
+      f(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value, decltype(axes)::value>);
     });
   }
   void record(Recorder &r) const override {
@@ -493,8 +512,8 @@ struct HeadNormRopeGrad final : Operator, HeadsCall {
   unsigned groups() const { return grid.x * grid.y; }
   size_t workspace() const override { return dw[0] || dw[1] ? (size_t)groups() * 2 * a.dim * sizeof(float) : 0; }
   template <class F> void with_kernel(F &&f) const {
-    with_form(dtype, pack, interleaved, stream(), [&](auto element, auto v, auto paired, auto past) {
-      f(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value>);
+    with_form(dtype, pack, interleaved, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
+      f(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value, decltype(axes)::value>);
     });
   }
   void record(Recorder &r) const override {
