@@ -367,9 +367,11 @@ typedef struct fc_page_map {
  *   (y[i], y[i + R/2]), interleaved: (y[2i], y[2i + 1]);  (a, b) -> (a c - b s, b c + a s).
  * In 32 bits, rounded once.  Keys go to k_out, or, with values as they are, to row slots[t] of the caches (page slots[t] / P, place
  * slots[t] mod P); slots outside the cache, -1 among them, are skipped; slots of one call are distinct.  A position or an axis outside
- * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides). */
+ * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides).
+ * At most 255 axes and 2^31-1 places of the cache (FC_E_LIMIT).  Rows are read 16 bytes at a time; where D/2, R/2, a stride or an
+ * alignment does not allow it fewer, and then D is at most 128 times the elements of a read (FC_E_UNSUPPORTED). */
 typedef struct fc_head_norm_rope {
-  fc_tensor q;            /* [T, Hq, D]: f32, f16 or bf16; D <= 512 */
+  fc_tensor q;            /* [T, Hq, D]: f32, f16 or bf16; D even, at most 512 */
   fc_tensor k;            /* [T, Hk, D] */
   fc_tensor q_weight;     /* [D] of the same type, or absent */
   fc_tensor k_weight;
@@ -405,7 +407,8 @@ typedef struct fc_head_norm_rope_grad {
  * [max(0, len - window), len), len = lengths[b] (window 0: all), at place j mod P of page table[b][j / P]; keys on pages that are
  * outside the cache or the table are not there.  Query head h reads key head h / (Hq / Hk).
  *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
- * A request without keys gets zeros and -inf.  What lies in the pages past a request's length is not looked at, whatever it holds. */
+ * A request without keys gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key head) are counted in 31 bits
+ * (FC_E_LIMIT).  What lies in the pages past a request's length is not looked at, whatever it holds. */
 typedef struct fc_paged_attention {
   fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
   fc_tensor k_cache;      /* [pages, P, Hk, D], in any order of strides with D innermost; rows 16-byte aligned */
