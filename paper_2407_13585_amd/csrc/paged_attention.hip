@@ -15,7 +15,8 @@
 //
 // The keys of all requests and key heads are one long row of units of 128 (64) keys, of which every workgroup takes an equal share,
 // whatever the lengths are: what is long is split, what is short is taken together.  Pieces of a split row go to scratch; the
-// workgroup that is the last of a row to be done joins them in their order, in two steps where they are many.
+// workgroup that is the last of a row to be done joins them in their order, in two steps where they are many.  Where all rows are short and
+// they are many, a wave takes one at a time instead, and nothing is exchanged at all.
 #include "operators.hpp"
 
 #include <algorithm>
@@ -28,6 +29,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr unsigned kMostDim = 256;
 constexpr unsigned kLongRow = 16;          // units
+constexpr unsigned kShortRow = 2;          // units
 constexpr int kColumns = 16;               // query heads of a group that are taken together
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
@@ -42,6 +44,7 @@ struct AttentionArgs {
   long long k_page, k_place, k_head, v_page, v_place, v_head;
   unsigned requests, kv_heads, group, tiles, dim, page, pages, width, window;      // tiles: a group's heads, 16 at a time
   unsigned workers, streams;               // workgroups; as many of them as keep the memory busy with long rows
+  bool wide_out;                           // rows of out are 16-byte aligned
   unsigned page_factor, page_shift;        // n / (page / 16) = n * page_factor >> page_shift, n below 2^30
   float scale;                             // times log2(e)
 };
@@ -106,26 +109,39 @@ template <class T> __device__ __forceinline__ Span span_of(const AttentionArgs &
 // This workgroup's share of all units: units [at, end) of the row, the first of them `offset` units into request `request`.
 struct Share {
   unsigned at, end, offset, share, request;
+  bool by_wave;                            // every row is short, and they are many: a wave takes a row at a time
 };
 
 template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs &a, unsigned worker) {
-  __shared__ unsigned sums[kWaves], found_offset, found;
+  __shared__ unsigned sums[kWaves], found_offset, found;     // the top bit of a sum, which is below 2^31: a row is long
   const unsigned rows = a.kv_heads * a.tiles, each = (a.requests + kThreads - 1) / kThreads;
   const unsigned b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
-  unsigned mine = 0;
-  for (unsigned b = b0; b < b1; ++b) mine += span_of<T>(a, a.lengths[b]).units;
+  unsigned mine = 0, most = 0;
+  for (unsigned b = b0; b < b1; ++b) {
+    const unsigned units = span_of<T>(a, a.lengths[b]).units;
+    mine += units;
+    most = max(most, units);
+  }
   mine *= rows;
   const unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)mine);
-  if (lane_id() == kWave - 1) sums[wave_id()] = upto;
+  const unsigned is_long = __any(most > kShortRow) ? 0x80000000u : 0u;
+  if (lane_id() == kWave - 1) sums[wave_id()] = upto | is_long;
   __syncthreads();
-  unsigned before = 0, total = 0;
+  unsigned before = 0, total = 0, any_long = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave_id()) before += sums[w];
-    total += sums[w];
+    const unsigned sum = sums[w] & 0x7fffffffu;
+    any_long |= sums[w] ^ sum;
+    if (w < wave_id()) before += sum;
+    total += sum;
   }
   Share s;
   total = uniform(total);
+  // a row costs a workgroup about 6 us from its first page to its result, whatever its length.  Where none is longer than two units and they are
+  // more than the workgroups, a wave takes a whole row, which exchanges nothing and hides the others' waits (93 requests of 25 keys, 11 key heads,
+  // 192 elements of 16 bits 12 us, 26 by workgroups; 256 of 256 keys, 8 key heads of 128 48 us and 54); longer rows of unequal length
+  // would leave waves idle (200 of up to 500 keys 57 us, 51 by workgroups), few rows all but a few (64 of 256 keys 21 us and 16.5)
+  s.by_wave = uniform(any_long) == 0 && a.requests * rows > a.workers;
   // long rows keep a compute unit's memory pipe full with few workgroups, and the fewer they are the less is joined; short ones leave
   // gaps that others fill
   const unsigned workers = total >= kLongRow * a.requests * rows ? a.streams : a.workers;
@@ -417,15 +433,15 @@ template <class T, int Dim, bool Even> struct Wave {
     }
   }
 
-  // The steps at j0, j0 + kUnit, .. below `end`.  The keys of the next step are asked for once this one's are used up, its values likewise,
+  // The steps at j0, j0 + step, .. below `end`.  The keys of the next step are asked for once this one's are used up, its values likewise,
   // and the pages two steps ahead: steps past the end ask for nothing.
-  __device__ __forceinline__ void run(unsigned j0, unsigned end) {
+  __device__ __forceinline__ void run(unsigned j0, unsigned end, unsigned step) {
     if (j0 >= end) return;
-    Where now = locate(j0), next = locate(j0 + kUnit<T>);
+    Where now = locate(j0), next = locate(j0 + step);
     load_keys(now);
     load_values(now);
     for (;;) {
-      Where after = locate(next.j0 + kUnit<T>);
+      Where after = locate(next.j0 + step);
       float p[kSub][4];
       weigh(now, p);
       const bool more = next.j0 < end;
@@ -438,6 +454,29 @@ template <class T, int Dim, bool Even> struct Wave {
     }
   }
 };
+
+// A row that one wave has done: its lanes write what they hold.
+template <class W, class T> __device__ __forceinline__ void write_wave(const AttentionArgs &a, const W &w, unsigned b, unsigned head0, unsigned count, float l, T *) {
+  if (w.r >= count) return;
+  const unsigned head = head0 + w.r;
+  T *to = reinterpret_cast<T *>(a.out) + b * a.out_request + head * a.out_head;
+  const float by_l = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < W::kW; j += W::kPart)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned d = w.d_of(i, j);
+      if (d >= a.dim) continue;
+      typename W::Part x;
+#pragma unroll
+      for (int e = 0; e < W::kPart; ++e) x[e] = (T)(w.o[j + e][i] * by_l);
+      if (a.wide_out) store_vec<T, W::kPart, false>(to + d, x);
+      else
+#pragma unroll
+        for (int e = 0; e < W::kPart; ++e) to[d + e] = x[e];
+    }
+  if (a.lse && w.g == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : (w.m - (float)Kind<T>::kShift + __log2f(l)) * kLn2;
+}
 
 template <class T> __device__ __forceinline__ void write_result(const AttentionArgs &a, unsigned b, unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) {
   Vec<T, 4> x;
@@ -552,6 +591,19 @@ __global__ __launch_bounds__(kThreads, Dim == 256 ? 1 : Dim == 128 ? (Even && si
       write_result<T>(a, b, i / (a.dim / 4), i % (a.dim / 4) * 4, Vec<float, 4>{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f, 0.0f);
   }
   Share s = share_of<T>(a, worker);
+  if (__builtin_expect(s.by_wave, 0)) {
+    for (unsigned turn = worker * kWaves + uniform((unsigned)wave_id()); turn < a.requests * rows; turn += a.workers * kWaves) {
+      const unsigned b = turn / rows, row = turn - b * rows;
+      const Span span = span_of<T>(a, load_scalar(a.lengths + b));
+      if (span.units == 0) continue;
+      const unsigned kv = row / a.tiles, head0 = kv * a.group + row % a.tiles * kColumns;
+      const unsigned count = min((unsigned)kColumns, (kv + 1) * a.group - head0);
+      Wave<T, Dim, Even> w(a, span, b, kv, head0, count);
+      w.run(span.from, span.end, Kind<T>::kKeys);
+      write_wave(a, w, b, head0, count, column_sum(w.l), (T *)nullptr);
+    }
+    return;
+  }
   const unsigned share_begin = s.at;
   while (s.at < s.end) {
     const unsigned b = s.request;
@@ -561,7 +613,7 @@ __global__ __launch_bounds__(kThreads, Dim == 256 ? 1 : Dim == 128 ? (Even && si
     const unsigned kv = row / a.tiles, head0 = kv * a.group + row % a.tiles * kColumns;
     const unsigned count = min((unsigned)kColumns, (kv + 1) * a.group - head0);
     Wave<T, Dim, Even> w(a, span, b, kv, head0, count);
-    w.run(span.from + unit0 * kUnit<T> + uniform((unsigned)wave_id()) * Kind<T>::kKeys, min(span.end, span.from + unit1 * kUnit<T>));
+    w.run(span.from + unit0 * kUnit<T> + uniform((unsigned)wave_id()) * Kind<T>::kKeys, min(span.end, span.from + unit1 * kUnit<T>), kUnit<T>);
     const float total = column_sum(w.l);
     __syncthreads();                                         // the row before is read
     if (g == 0) { tops[wave_id()][r] = w.m; totals[wave_id()][r] = total; }
@@ -723,6 +775,7 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
     a.page_factor = (unsigned)(((1ull << a.page_shift) + d - 1) / d);
   }
   a.scale = (float)(n.scale * (double)kLog2e);
+  a.wide_out = common_alignment(n.out, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) == 16;
   const int64_t units = ceil_div((uint64_t)a.width * a.page, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;      // of a request: one more where a window starts inside
   if (units * requests * kv * a.tiles > 0x7fffffff) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
   op->most_units = (unsigned)(units * requests * kv * a.tiles);

@@ -562,6 +562,51 @@ def test_attention_on_strided_tensors_and_without_lse():
     check_attention(same, "bf16")
 
 
+def many_short(dtype, seed, requests=300, longest=None):
+    """More rows than workgroups are resident, none longer than two steps of a workgroup, unless `longest` says so."""
+    rng = np.random.default_rng(seed)
+    lengths = rng.integers(0, 129 if dtype == "f32" else 257, requests)
+    lengths[:len(LENGTHS)] = np.minimum(LENGTHS, 128 if dtype == "f32" else 256)
+    if longest:
+        lengths[requests // 2] = longest
+    return lengths
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dim,page,heads_first", [(64, 16, False), (40, 24, True), (128, 16, True), (128, 5, False), (96, 32, False), (192, 48, False), (256, 7, True)])
+def test_attention_of_many_short_rows(dtype, dim, page, heads_first):
+    s = attention_case(many_short(dtype, dim + page), 8, 4, dim, page, dtype, seed=dim, heads_first=heads_first)
+    check_attention(s, dtype)
+    if dim in (64, 128):
+        check_attention(s, dtype, window=37)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hk", [(4, 4), (17, 1), (66, 2)])
+def test_attention_of_many_short_rows_with_groups_of_any_size(dtype, hq, hk):
+    check_attention(attention_case(many_short(dtype, hq, requests=1200 // (hk * -(-hq // hk // 16))), hq, hk, 64, 16, dtype, seed=hq), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_many_short_rows_and_one_that_is_not(dtype):
+    check_attention(attention_case(many_short(dtype, 1, longest=1500), 8, 4, 64, 16, dtype, seed=21), dtype)
+
+
+def test_attention_of_many_short_rows_into_rows_that_are_not_aligned_and_over_missing_pages():
+    import torch
+    import paper_2407_13585_amd as fc
+    s = attention_case(many_short("bf16", 2), 8, 4, 64, 16, "bf16", seed=22)
+    holes = torch.rand(s["table"].shape, generator=torch.Generator().manual_seed(23)).cuda() < 0.3
+    s["table"][holes] = -1
+    want = attention_want(s, 0.125, 0)
+    out = torch.full((300, 8, 65), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty((300, 8), device="cuda")
+    run([fc.PagedAttention(out=out[:, :, 1:], lse=lse, **s)])
+    near(host(out[:, :, 1:]), want[0], 2.0 ** -8 * np.abs(want[0]) + 2.0 ** -14 * (1 + want[3]))
+    near(host(lse), want[1], 1e-5 * (1 + np.abs(want[1])))
+    assert (out[:, :, 0] == 9).all()
+
+
 def test_attention_gives_the_same_bits_every_time():
     s = attention_case([3000, 1, 777], 8, 2, 128, 16, "bf16", seed=14, poison=False)
     first = [host(t) for t in attention_raw(s)]
