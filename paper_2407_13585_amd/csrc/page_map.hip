@@ -15,6 +15,7 @@ namespace fc {
 namespace {
 
 constexpr int kPerThread = 4;                      // requests of a thread, and tokens
+constexpr unsigned kRequestsOfGroup = 32;          // pages given back ask for workgroups too: a step of 2231 requests, half of which leave, 9.8 us, 10.8 without
 constexpr int kMany = 1024, kFew = 256;            // threads of a workgroup
 constexpr int kChunk = kMany * kPerThread;         // requests that a workgroup of many threads sums at once
 
@@ -337,9 +338,9 @@ struct PageMap final : Operator {
     return a.requests <= (unsigned)kChunk ? 0 : chunks() * (4 * sizeof(unsigned) * kChunk + sizeof(long long) + sizeof(Sums));
   }
   void record(Recorder &r) const override {
-    // as many workgroups as the tokens ask for, one for each compute unit at most: each sums all requests first.  What is given back,
-    // which only the device knows, they share.
-    auto groups = [&](int threads) { return std::min(std::max(ceil_div(a.tokens, threads * kPerThread), 1u), 256u); };
+    // as many workgroups as the tokens ask for, or the pages given back, which only the device knows, may ask for; one for each compute unit at
+    // most: each sums all requests first
+    auto groups = [&](int threads) { return std::min(std::max({ceil_div(a.tokens, threads * kPerThread), ceil_div(a.requests, kRequestsOfGroup), 1u}), 256u); };
     if (a.requests <= (unsigned)(kFew * kPerThread) && a.tokens <= 256u * kFew * kPerThread) {
       r.launch(&page_map_kernel<kFew>, groups(kFew) + 1, kFew, a);
       return;
