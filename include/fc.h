@@ -343,7 +343,8 @@ typedef struct fc_operator {
  *   (positions[t] >= lengths_after[r], or its entry is negative).  Past the last token: -1, 0, -1.
  *   cursor_after: the cursor of the next step; unplaced[0]: tokens of all requests that found no page.
  * cursor, lengths and new_tokens are not written, so a step that is run again gives the same; the ring and the table
- * are written in place.  Tokens beyond the extent of slots have no entry. */
+ * are written in place.  Tokens beyond the extent of slots have no entry.  Where the new tokens are 2^31 or more together,
+ * row_start stays at 2^31-1. */
 typedef struct fc_page_map {
   int32_t   page_size;
   fc_tensor lengths;        /* i32 [B] */

@@ -199,9 +199,8 @@ __device__ __forceinline__ unsigned last_not_above(const unsigned *starts, unsig
 // The share of workgroup `group` of `groups` in the tokens, and in the pages given back.
 template <int Threads>
 __device__ __forceinline__ void fill(const PageMapArgs &a, const Ring &ring, Sums all, const Starts &of, unsigned group, unsigned groups) {
-  // also tokens that have no entry: the first on a page still enters it
-  const unsigned live = token_of(all.tokens), last = max(a.tokens, live), stride = groups * Threads;
-  for (unsigned n = group * Threads + threadIdx.x; n < (last + kPerThread - 1) / kPerThread; n += stride) {
+  const unsigned live = token_of(all.tokens), stride = groups * Threads;
+  for (unsigned n = group * Threads + threadIdx.x; n < (a.tokens + kPerThread - 1) / kPerThread; n += stride) {
     const unsigned t0 = n * kPerThread;
     Vec<int, kPerThread> positions, requests;
     Vec<long long, kPerThread> slots;
@@ -259,6 +258,12 @@ __device__ __forceinline__ void fill(const PageMapArgs &a, const Ring &ring, Sum
       }
   }
   if (a.entries == 0) return;
+  // the pages of tokens that have no entry, which nobody above has seen: all pages taken, some a second time
+  if (live > a.tokens)
+    for (unsigned i = group * Threads + threadIdx.x; i < min(all.taken, ring.available); i += stride) {
+      const unsigned r = last_not_above(of.first, a.requests, i);
+      a.table[(long long)r * a.table_stride + pages_of(a, of.length[r]) + (i - of.first[r])] = a.pool[Ring::place(a, ring.head, i)];
+    }
   for (unsigned i = group * Threads + threadIdx.x; i < min(all.given, a.entries); i += stride) {
     const unsigned r = last_not_above(of.behind, a.requests, i);
     const unsigned begin = of.behind[r], given = (r + 1 < a.requests ? of.behind[r + 1] : all.given) - begin, goal = pages_of(a, of.length[r]) - given;

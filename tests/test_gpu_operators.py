@@ -114,6 +114,33 @@ def check_map(case, repeat=1, table_room=0):
     return want
 
 
+def check_map_counted(case):
+    """The same where the oracle would count one by one and its row_start would not fit: computed on fewer tokens, with the same pages."""
+    import torch
+    import paper_2407_13585_amd as fc
+    size = 1 << 20                                              # the oracle's pages are that much smaller
+    small = {**case, "page_size": case["page_size"] // size, "lengths": -(-case["lengths"].astype(np.int64) // size),
+             "new_tokens": -(-(case["lengths"].astype(np.int64) + case["new_tokens"]) // size) - -(-case["lengths"].astype(np.int64) // size)}
+    want = O.page_map(**small)
+    requests = len(case["lengths"])
+    ins = {k: gpu(case[k]) for k in ("lengths", "new_tokens", "pool", "cursor", "table")}
+    outs = {k: torch.full((n,), -77, dtype=t, device="cuda") for k, n, t in (
+        ("lengths_after", requests, torch.int32), ("row_start", requests + 1, torch.int32), ("slots", case["tokens"], torch.int64),
+        ("positions", case["tokens"], torch.int32), ("request", case["tokens"], torch.int32), ("cursor_after", 2, torch.int64), ("unplaced", 1, torch.int64))}
+    run([fc.PageMap(page_size=case["page_size"], **ins, **outs)])
+    assert np.array_equal(host(ins["table"]), want["table"]) and np.array_equal(host(ins["pool"]), want["pool"])
+    assert np.array_equal(host(outs["cursor_after"]), want["cursor_after"])
+    sums = np.concatenate([[0], np.cumsum(case["new_tokens"].astype(np.int64))])
+    assert np.array_equal(host(outs["row_start"]), np.minimum(sums, 2 ** 31 - 1))
+    whole = case["lengths"].astype(np.int64) + case["new_tokens"]
+    held = (want["table"] >= 0).sum(1).astype(np.int64) * case["page_size"]
+    assert np.array_equal(host(outs["lengths_after"]), np.minimum(whole, held)) and host(outs["unplaced"])[0] == (whole - np.minimum(whole, held)).sum()
+    first = np.arange(case["tokens"]) + case["lengths"][0]
+    assert np.array_equal(host(outs["positions"]), first) and (host(outs["request"]) == 0).all()
+    assert np.array_equal(host(outs["slots"]), want["table"][0][first // case["page_size"]].astype(np.int64) * case["page_size"] + first % case["page_size"])
+    return want
+
+
 @pytest.mark.parametrize("requests", [1, 2, 63, 64, 65, 257, 1000, 1025, 4095, 4096, 4097, 9001])
 @pytest.mark.parametrize("kind", ["step", "mixed"])
 def test_page_map_of_many_and_few_requests(requests, kind):
@@ -172,6 +199,15 @@ def test_page_map_of_a_few_very_long_requests():
     case = dict(page_size=1 << 20, lengths=np.array([2 ** 31 - 5, 0, 5], np.int32), new_tokens=np.array([4, 1, -5], np.int32),
                 pool=np.arange(3000, dtype=np.int32), cursor=np.array([2 ** 40, 2 ** 40 + 7], np.int64), table=np.full((3, 2100), 1 << 12, np.int32), tokens=9)
     check_map(case)
+
+
+def test_page_map_of_more_tokens_than_can_be_counted():
+    # four requests ask for 2^31-1 tokens each; few of them have an entry, and all pages there are get entered
+    case = dict(page_size=1 << 22, lengths=np.array([7, 0, 1 << 22, 3], np.int32), new_tokens=np.array([2 ** 31 - 1 - 7, 2 ** 31 - 1, 2 ** 31 - 1 - (1 << 22), 2 ** 31 - 4], np.int32),
+                pool=np.arange(1500, dtype=np.int32), cursor=np.array([3, 1400], np.int64), table=np.full((4, 600), -1, np.int32), tokens=33)
+    case["table"][[0, 2, 3], 0] = [1450, 1451, 1452]
+    want = check_map_counted(case)
+    assert (want["table"] >= 0).sum() == 3 + 1397
 
 
 # --------------------------------------------------------------------------- norm and rotation
