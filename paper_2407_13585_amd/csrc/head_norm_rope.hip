@@ -306,8 +306,10 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
         g[1][i] = p.turned ? g1 * c[i] - g0 * s[i] : g1;
       }
       if (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
-        // the sums are taken by all lanes of a row together: a row is of q or of k as a whole
-        const float r = 1.0f / sqrtf(lanes_sum(sum_of_products(x, x), (int)a.lanes_log2) * by_dim + a.eps);
+        // the sums are taken by all lanes of a row together: a row is of q or of k as a whole.  A row that no head has is zeros, whose norm
+        // is not finite where eps is 0: it must leave the weights' sums alone.
+        const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
+        const float r = n.live ? 1.0f / sqrtf(square * by_dim + a.eps) : 0.0f;
         float w[2][V];
         unpack(either(n.is_q, wq, wk), p, w);
 #pragma unroll
@@ -315,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             x[k][i] *= r;
-            const float dw = g[k][i] * x[k][i];              // zero where the row is not live
+            const float dw = g[k][i] * x[k][i];
             dq[k][i] += n.is_q ? dw : 0.0f;
             dk[k][i] += n.is_q ? 0.0f : dw;
             g[k][i] *= w[k][i];

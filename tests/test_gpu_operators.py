@@ -395,6 +395,15 @@ def test_gradient_without_a_norm_and_in_place(dtype):
     check_grad(heads_case(77, 6, 3, 96, 48, dtype, seed=2), dtype, in_place=True)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hk", [(3, 1), (9, 2)])
+def test_norm_and_gradient_with_an_eps_of_zero(dtype, hq, hk):
+    # rows of a wave that no head has are zeros, whose norm is not finite without eps: nothing of them may reach the weights' gradients
+    s = heads_case(11, hq, hk, 64, 64, dtype, seed=hq)
+    check_heads(s, dtype, eps=0.0)
+    check_grad(s, dtype, eps=0.0)
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_gradient_against_differences(interleaved):
     # along a random direction, central differences of the definition: their own error is of second order in the step
