@@ -9,6 +9,7 @@
 #include "operators.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace fc {
 
@@ -450,7 +451,7 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
   } else if (present(positions) || present(axis_of)) {
     c.fail(FC_E_ARG, "positions and axis_of go with cos_sin");
   }
-  if (c.ok() && !(eps >= 0)) c.fail(FC_E_ARG, "eps must not be negative");
+  if (c.ok() && !(eps >= 0 && std::isfinite((float)eps))) c.fail(FC_E_ARG, "eps must be finite, in 32 bits too, and not negative");
   if (c.ok() && (dim < 2 || dim % 2 || dim > (int64_t)kMostDim)) c.fail(FC_E_UNSUPPORTED, "heads have an even number of elements, at most 512");
   if (c.ok() && tokens * (q.shape[1] + k.shape[1]) > (int64_t)1 << 40) c.fail(FC_E_LIMIT, "too many heads");
   if (!c.ok()) return c.code();

@@ -730,7 +730,7 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   if (page < 1) return c.fail(FC_E_ARG, "k_cache: pages without places").code();
   if (kv < 1 || heads % kv) return c.fail(FC_E_ARG, "the heads of q must be a multiple of those of the cache").code();
   if (dim < 8 || dim % 8 || dim > (int64_t)kMostDim) return c.fail(FC_E_UNSUPPORTED, "heads have a multiple of 8 elements, at most 256").code();
-  if (!std::isfinite(n.scale)) return c.fail(FC_E_ARG, "scale must be finite").code();
+  if (!std::isfinite((float)(n.scale * (double)kLog2e))) return c.fail(FC_E_ARG, "scale must be finite, in 32 bits too").code();
   if (n.window < 0) return c.fail(FC_E_ARG, "window must not be negative").code();
   for (const fc_tensor *t : {&n.q, &n.k_cache, &n.v_cache})
     if (requests && pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16)

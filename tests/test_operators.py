@@ -112,6 +112,8 @@ REFUSED = [
     ("FC_E_ARG", lambda: heads(axis_of=T("int32", 31))),
     ("FC_E_ARG", lambda: heads(eps=-1.0)),
     ("FC_E_ARG", lambda: heads(eps=math.nan)),
+    ("FC_E_ARG", lambda: heads(eps=1e39)),                                                 # infinite in 32 bits
+    ("FC_E_ARG", lambda: heads(True, eps=math.inf)),
     ("FC_E_ARG", lambda: heads(q_out=T("bfloat16", 7, 4, 64, stride=(0, 64, 1)))),
     ("FC_E_ARG", lambda: heads(q_out=T("bfloat16", 7, 4, 64, stride=(256, 64, 2)))),
     ("FC_E_ARG", lambda: heads(q_out=T("bfloat16", 7, 5, 64))),
@@ -148,6 +150,7 @@ REFUSED = [
     ("FC_E_ARG", lambda: attention(window=-1)),
     ("FC_E_ARG", lambda: attention(scale=math.inf)),
     ("FC_E_ARG", lambda: attention(scale=math.nan)),
+    ("FC_E_ARG", lambda: attention(scale=-1e39)),
     ("FC_E_ARG", lambda: attention(k_cache=T("bfloat16", 9, 0, 2, 64), v_cache=T("bfloat16", 9, 0, 2, 64))),
     ("FC_E_UNSUPPORTED", lambda: attention(dim=264)),
     ("FC_E_UNSUPPORTED", lambda: attention(dim=60)),
