@@ -5,7 +5,11 @@
 // whose i-th elements are rotated together: (y[i], y[i + R/2]) lie R/2 apart, (y[2i], y[2i+1]) are the even and the odd elements of
 // two packs in a row; behind the rotated part the packs just follow each other.  So nothing is exchanged between lanes but the sum of
 // squares, and the row is read once and written once.  A wave takes one token after the other with some of its heads, so that
-// the token's cosines and sines and the weights are read once and stay in registers.
+// the token's cosines and sines and the weights are read once and stay in registers.  Memory bounds it where it is large, the launch and a chain
+// of reads (position, angles, result) where it is small:
+//   16384 tokens of 40 heads of 128 (bf16, 338 MB) 61.2 us, 5.5 TB/s; 5003 tokens of 16 heads of 80 with three axes (f16, 27 MB) 10.9 us;
+//   64 tokens into the cache 5.9 us; the gradient of the first (505 MB) with the sum of the weights' gradients 96.7 us, 5.2 TB/s, of 1237
+//   tokens of 12 heads of 64 (f32, 11.6 MB) 10.1 us, a third of them the second launch.
 #include "operators.hpp"
 
 #include <algorithm>
@@ -131,7 +135,7 @@ __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
 
 // Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  With
 // one axis a lane reads them from the one row of the token.  With several the lanes of the wave read a pair each and share them through LDS, as
-// every row of the wave needs the same (5003 tokens of 16 heads with three axes: 10.9 us; 14.0 where each lane read its pairs from all rows).
+// every row of the wave needs the same (5003 tokens of 16 heads with three axes 10.9 us; 14.0 where each lane read its pairs from all rows).
 // shared: kMostDim floats of the wave.
 template <bool Axes, int V, bool Interleaved>
 __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned axes, unsigned t, float *shared, float (&c)[V], float (&s)[V]) {
@@ -416,10 +420,10 @@ struct HeadsCall {
   dim3 grid;
   unsigned heads() const { return a.heads[0] + a.heads[1] + a.heads[2]; }
   // What is read and written passes the caches where they would not hold it until it is used (16384 tokens of 40 heads 70 us through them,
-  // 63 past them).
+  // 61 past them; 4000 tokens, 41 MB, 18.7 either way).
   bool stream() const { return (unsigned long long)a.tokens * heads() * a.dim * size_of_dtype(dtype) >= 32u << 20; }
   // How the heads of a token are shared among waves (grid.y), and the workgroups that are then needed, as many as are resident at once at
-  // most: a second round of a few lasts as long as the first (the gradient of 16384 tokens on 768 workgroups 95 us, 1024 117).  A wave takes
+  // most: a second round of a few lasts as long as the first (the gradient of 16384 tokens on 768 workgroups 97 us, 1024 120).  A wave takes
   // all heads of a token, unless that leaves compute units without work.
   template <class... P> void shape(void (*kernel)(P...)) {
     const unsigned resident = resident_workgroups(kernel, kThreads), most = resident ? resident : 768u;

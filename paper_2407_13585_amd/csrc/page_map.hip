@@ -6,8 +6,8 @@
 // reads of one token.  Up to 4096 requests every workgroup sums all of them for itself and keeps the sums in LDS, which makes a
 // step one launch (1024 threads a workgroup; 256 up to 1024 requests, whose barriers and scans are shorter); above, two kernels
 // leave the sums in scratch for the third.  What there is of each request is written by a workgroup of its own.
-//   64 requests, a token each: 5.9 us (a launch is about 4); 1000 requests, 60013 tokens: 7.1 us (7.9 with 1024 threads a workgroup);
-//   4096 requests, 2^20 tokens (17 MB): 11.4 us (17.8 with a token a thread).
+//   64 requests, a token each: 5.8 us (an empty launch is about 4); 1000 requests, 60013 tokens (1.2 MB): 7.0 us (7.6 with 1024 threads a workgroup);
+//   4096 requests, 2^20 tokens (17 MB): 11.5 us, 1.5 TB/s (17.8 with a token a thread): the sums, a search in LDS, a page and a store one behind another.
 #include "operators.hpp"
 
 namespace fc {
@@ -401,7 +401,8 @@ int make_page_map(const fc_page_map &a, std::unique_ptr<Operator> &out, std::str
   k.cursor_after = static_cast<long long *>(a.cursor_after.ptr);
   k.unplaced = static_cast<long long *>(a.unplaced.ptr);
   k.table_stride = a.table.stride[0];
-  k.wide = common_alignment(a.lengths, 4) == 4 && common_alignment(a.new_tokens, 4) == 4 && common_alignment(a.slots, 2) == 2 && common_alignment(a.positions, 4) == 4 && common_alignment(a.request, 4) == 4;
+  k.wide = common_alignment(a.lengths, 4) == 4 && common_alignment(a.new_tokens, 4) == 4 && common_alignment(a.slots, 2) == 2 &&
+           common_alignment(a.positions, 4) == 4 && common_alignment(a.request, 4) == 4;
   k.requests = (unsigned)requests;
   k.width = (unsigned)a.table.shape[1];
   k.page = (unsigned)a.page_size;

@@ -17,6 +17,11 @@
 // whatever the lengths are: what is long is split, what is short is taken together.  Pieces of a split row go to scratch; the
 // workgroup that is the last of a row to be done joins them in their order, in two steps where they are many.  Where all rows are short and
 // they are many, a wave takes one at a time instead, and nothing is exchanged at all.
+//
+// Reading the cache once bounds it where that is long, the launch and a chain of reads (lengths, page, keys, pieces) where it is not:
+//   one request of 131072 keys, 8 key heads of 128, 64 heads (bf16, 537 MB) 88 us, 6.1 TB/s; 64 requests of 1 to 8192 keys, 8 key heads of 128 (bf16)
+//   169 us, 6.3 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB) 33 us, 3.4 TB/s, where the six
+//   units of a workgroup are too few to hide its start and end; 4 requests of up to 300 keys, 2 key heads of 64 (f16) 6.9 us.
 #include "operators.hpp"
 
 #include <algorithm>
@@ -28,7 +33,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr unsigned kMostDim = 256;
-constexpr unsigned kLongRow = 16;          // units
+constexpr unsigned kLongRow = 8;           // units
 constexpr unsigned kShortRow = 2;          // units
 constexpr int kColumns = 16;               // query heads of a group that are taken together
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
@@ -143,7 +148,8 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
   // would leave waves idle (200 of up to 500 keys 57 us, 51 by workgroups), few rows all but a few (64 of 256 keys 21 us and 16.5)
   s.by_wave = uniform(any_long) == 0 && a.requests * rows > a.workers;
   // long rows keep a compute unit's memory pipe full with few workgroups, and the fewer they are the less is joined; short ones leave
-  // gaps that others fill
+  // gaps that others fill: one workgroup a compute unit and all that are resident take for a request of 131072 keys 88 and 102 us, 100 of 1000
+  // keys 75 and 84, 200 of up to 1000 89 and 84.5, 200 of up to 500 60 and 51
   const unsigned workers = total >= kLongRow * a.requests * rows ? a.streams : a.workers;
   s.share = max((total + workers - 1) / workers, 1u);
   s.at = (unsigned)min((unsigned long long)worker * s.share, (unsigned long long)total);
