@@ -218,6 +218,13 @@ struct Turn {
       : live(h < end), is_q(h < a.heads[0]), is_v(h >= a.heads[0] + a.heads[1]), head(is_q ? h : is_v ? h - a.heads[0] - a.heads[1] : h - a.heads[0]) {}
 };
 
+// 1 / sqrt(x) by the instruction (1 ulp; 5003 tokens of 16 heads 10.9 us, 11.3 by root and quotient), which takes what is below the normal numbers
+// for 0
+__device__ __forceinline__ float inverse_root(float x) {
+  if (__any(x < 0x1p-126f)) return 1.0f / sqrtf(x);
+  return __builtin_amdgcn_rsqf(x);
+}
+
 template <int V> __device__ __forceinline__ float sum_of_products(const float (&x)[2][V], const float (&y)[2][V]) {
   float s = 0.0f;
 #pragma unroll
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
       if (!n.is_v) {
         float w[2][V];
         unpack(either(n.is_q, wq, wk), p, w);
-        const float r = (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? 1.0f / sqrtf(square * by_dim + a.eps) : 1.0f;
+        const float r = (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? inverse_root(square * by_dim + a.eps) : 1.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float y0 = x[0][i] * r * w[0][i], y1 = x[1][i] * r * w[1][i];
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
         // the sums are taken by all lanes of a row together: a row is of q or of k as a whole.  A row that no head has is zeros, whose norm
         // is not finite where eps is 0: it must leave the weights' sums alone.
         const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
-        const float r = n.live ? 1.0f / sqrtf(square * by_dim + a.eps) : 0.0f;
+        const float root = inverse_root(square * by_dim + a.eps), r = n.live ? root : 0.0f;
         float w[2][V];
         unpack(either(n.is_q, wq, wk), p, w);
 #pragma unroll
