@@ -51,7 +51,7 @@ struct AttentionArgs {
   unsigned workers, streams;               // workgroups; as many of them as keep the memory busy with long rows
   bool wide_out;                           // rows of out are 16-byte aligned
   unsigned page_factor, page_shift;        // n / (page / 16) = n * page_factor >> page_shift, n below 2^30
-  float scale;                             // times log2(e)
+  float scale;
 };
 
 // What the types differ in.  kKeys: keys of a wave's step; kShift: the weights are held 2^kShift larger, which keeps the small ones
@@ -82,6 +82,10 @@ __device__ __forceinline__ void split(float p, _Float16 &high, _Float16 &low) {
   high = (_Float16)__builtin_amdgcn_cvt_pkrtz(p, 0.0f)[0];
   low = (_Float16)fmaxf(p - (float)high, 0x1p-24f);
 }
+
+// 2^shift e^x, x not above 0.  The difference from the maximum is taken before it is put into powers of 2, so that the rounding of large scores
+// cancels; a scale that is a power of 2 then leaves scores as exact as their products.
+__device__ __forceinline__ float exp_of(float x, float shift = 0.0f) { return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, shift)); }
 
 // over the lanes of a head: lane, lane ^ 16, lane ^ 32, lane ^ 48.  Swapping a register's odd rows of 16 lanes with another's even ones,
 // or its upper half with the other's lower one, leaves the two values that belong together in the two.
@@ -372,9 +376,15 @@ template <class T, int Dim, bool Even> struct Wave {
     float most = -__builtin_inff();
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
-      Acc score = {0.0f, 0.0f, 0.0f, 0.0f};
+      // in four sums where products are of 32 bits: the rounding of one long sum is most of the result's error, and four halve it
+      constexpr int kSums = sizeof(T) == 4 ? 4 : 1;
+      Acc part[kSums];
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c) score = mma(kf[u][c], q[c], score);
+      for (int c = 0; c < kSums; ++c) part[c] = Acc{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) part[c % kSums] = mma(kf[u][c], q[c], part[c % kSums]);
+      Acc score = part[0];
+      if constexpr (kSums == 4) score = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[u][i] = score[i] * a.scale;
     }
@@ -392,9 +402,9 @@ template <class T, int Dim, bool Even> struct Wave {
 #pragma unroll
       for (int i = 0; i < 4; ++i) most = fmaxf(most, p[u][i]);
     most = fmaxf(column_max(most), m);
-    const float top = most == -__builtin_inff() ? 0.0f : most, base = top - (float)Kind<T>::kShift;
+    const float top = most == -__builtin_inff() ? 0.0f : most;
     if (__any(most > m)) {                                   // of any head: the maxima settle after a few keys
-      const float keep = __builtin_amdgcn_exp2f(m - top);
+      const float keep = exp_of(m - top);
       m = most;
       l *= keep;
 #pragma unroll
@@ -404,7 +414,7 @@ template <class T, int Dim, bool Even> struct Wave {
     for (int u = 0; u < kSub; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[u][i] = __builtin_amdgcn_exp2f(p[u][i] - base);
+        p[u][i] = exp_of(p[u][i] - top, (float)Kind<T>::kShift);
         l += p[u][i];
       }
   }
@@ -481,7 +491,7 @@ template <class W, class T> __device__ __forceinline__ void write_wave(const Att
 #pragma unroll
         for (int e = 0; e < W::kPart; ++e) to[d + e] = x[e];
     }
-  if (a.lse && w.g == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : (w.m - (float)Kind<T>::kShift + __log2f(l)) * kLn2;
+  if (a.lse && w.g == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : w.m + (__log2f(l) - (float)Kind<T>::kShift) * kLn2;
 }
 
 template <class T> __device__ __forceinline__ void write_result(const AttentionArgs &a, unsigned b, unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) {
@@ -491,7 +501,7 @@ template <class T> __device__ __forceinline__ void write_result(const AttentionA
   T *to = reinterpret_cast<T *>(a.out) + b * a.out_request + head * a.out_head + d;
 #pragma unroll
   for (int i = 0; i < 4; ++i) to[i] = x[i];
-  if (a.lse && d == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : (m - (float)Kind<T>::kShift + __log2f(l)) * kLn2;
+  if (a.lse && d == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : m + (__log2f(l) - (float)Kind<T>::kShift) * kLn2;
 }
 
 // A piece: the weighted sums of the heads, then (m, l) of each.  It is written and read around the caches that compute units do not
@@ -570,13 +580,13 @@ template <class Slot, class Use> __device__ __forceinline__ void join(const Atte
       float most = m;
 #pragma unroll
       for (int k = 0; k < kTogether; ++k) most = fmaxf(most, e[k][0]);
-      const float base = most == -__builtin_inff() ? 0.0f : most, keep = __builtin_amdgcn_exp2f(m - base);
+      const float base = most == -__builtin_inff() ? 0.0f : most, keep = exp_of(m - base);
       m = most;
       l *= keep;
       sum *= keep;
 #pragma unroll
       for (int k = 0; k < kTogether; ++k) {
-        const float f = __builtin_amdgcn_exp2f(e[k][0] - base);
+        const float f = exp_of(e[k][0] - base);
         l += e[k][1] * f;
         if (p + k < n) sum += x[k] * f;
       }
@@ -643,7 +653,7 @@ __global__ __launch_bounds__(kThreads, Dim == 256 ? 1 : Dim == 128 ? (Even && si
       Vec<float, 4> x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int n = 0; n < kWaves; ++n) {
-        const float f = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(tops[n][head] - most);
+        const float f = most == -__builtin_inff() ? 0.0f : exp_of(tops[n][head] - most);
         sum_l += totals[n][head] * f;
         x += *reinterpret_cast<const Vec<float, 4> *>(&sums[n][head][d]) * f;
       }
@@ -736,7 +746,7 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   if (page < 1) return c.fail(FC_E_ARG, "k_cache: pages without places").code();
   if (kv < 1 || heads % kv) return c.fail(FC_E_ARG, "the heads of q must be a multiple of those of the cache").code();
   if (dim < 8 || dim % 8 || dim > (int64_t)kMostDim) return c.fail(FC_E_UNSUPPORTED, "heads have a multiple of 8 elements, at most 256").code();
-  if (!std::isfinite((float)(n.scale * (double)kLog2e))) return c.fail(FC_E_ARG, "scale must be finite, in 32 bits too").code();
+  if (!std::isfinite((float)n.scale)) return c.fail(FC_E_ARG, "scale must be finite, in 32 bits too").code();
   if (n.window < 0) return c.fail(FC_E_ARG, "window must not be negative").code();
   for (const fc_tensor *t : {&n.q, &n.k_cache, &n.v_cache})
     if (requests && pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16)
@@ -780,7 +790,7 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
     a.page_shift = 31 + s;
     a.page_factor = (unsigned)(((1ull << a.page_shift) + d - 1) / d);
   }
-  a.scale = (float)(n.scale * (double)kLog2e);
+  a.scale = (float)n.scale;
   a.wide_out = common_alignment(n.out, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) == 16;
   const int64_t units = ceil_div((uint64_t)a.width * a.page, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;      // of a request: one more where a window starts inside
   if (units * requests * kv * a.tiles > 0x7fffffff) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();

@@ -607,6 +607,21 @@ def test_attention_on_strided_tensors_and_without_lse():
     check_attention(same, "bf16")
 
 
+@pytest.mark.parametrize("dim,page", [(64, 16), (192, 48), (256, 5)])
+def test_attention_of_32_bits_keeps_its_precision(dim, page):
+    """Root mean square of the error, relative to that of the result.
+
+    A score of n = dim products, its own size 2 here, is off by 2 * 2^-24 sqrt(n / 6) where they are summed one by one (7.8e-7 for 256), and by half of
+    it in four sums; weights are off by as much of themselves, and the output, a sum of values of either sign, by as much of its size.
+    With 2^-23 for the powers, their sum and the quotient: 5.1e-7 at most for 256."""
+    s = attention_case([1728, 900, 333], 20, 5, dim, page, "f32", seed=dim, sharp=2.0)
+    out, lse = check_attention(s, "f32")
+    ref, ref_lse = attention_want(s, dim ** -0.5, 0)[:2]
+    rms = lambda x: np.sqrt(np.mean(np.square(x)))  # noqa: E731
+    assert rms(out - ref) <= (2.0 ** -24 * math.sqrt(dim / 6) + 2.0 ** -23) * rms(ref)
+    assert rms(lse - ref_lse) <= 2.0 ** -24 * rms(ref_lse)
+
+
 def many_short(dtype, seed, requests=300, longest=None):
     """More rows than workgroups are resident, none longer than two steps of a workgroup, unless `longest` says so."""
     rng = np.random.default_rng(seed)
