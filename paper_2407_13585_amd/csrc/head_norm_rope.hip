@@ -1,9 +1,9 @@
 // Norm of query and key heads with the rotation by position in the same pass, into tensors or into the cache, and its gradient
 // (include/fc.h, fc_head_norm_rope).
 //
-// One head of one token is a row of D elements.  2^log2 neighbouring lanes hold a row, each of them two packs of V elements
-// whose i-th elements are rotated together: (y[i], y[i + R/2]) lie R/2 apart, (y[2i], y[2i+1]) are the even and the odd elements of
-// two packs in a row; behind the rotated part the packs just follow each other.  So nothing is exchanged between lanes but the sum of
+// One head of one token is a row of D elements.  2^log2 neighbouring lanes hold a row, each of them two packs of V elements that hold the
+// elements of its pairs: (y[i], y[i + R/2]) lie in packs that are R/2 apart, (y[2i], y[2i+1]) side by side in one; behind the rotated part
+// and for pairs side by side the packs are half of what there is apart.  So nothing is exchanged between lanes but the sum of
 // squares, and the row is read once and written once.  A wave takes one token after the other with some of its heads, so that
 // the token's cosines and sines and the weights are read once and stay in registers.  Memory bounds it where it is large, the launch and a chain
 // of reads (position, angles, result) where it is small:
@@ -44,16 +44,28 @@ struct HeadsArgs {
   bool wide_angles;                 // rows of cos_sin are aligned for packs
 };
 
-// Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.
+// Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.  The packs of neighbouring lanes lie side by side, so that
+// an instruction reads whole lines (6966 tokens of 16 heads of 256, f32, half of them turned, neighbours paired, 46 us; 55 with a lane's two packs in a row).
 template <int V, bool Interleaved> struct Place {
-  unsigned at[2], pair;             // pair: of the first elements
-  bool any, turned;
+  // the i-th pair is of pack i / kOfPack; one element a pack is half a pair
+  static constexpr bool kApart = Interleaved && V > 1;               // the packs have pairs of their own
+  static constexpr int kOfPack = kApart ? V / 2 : V;
+  static constexpr int kAngles = kOfPack < 4 ? kOfPack : 4;          // angles that are read at once
+  unsigned at[2];
+  bool any, turned[2];
   __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
     any = 2 * V * chunk < dim;
-    turned = V * chunk < half;
-    pair = V * chunk;
-    at[0] = turned && !Interleaved ? V * chunk : 2 * V * chunk;
-    at[1] = turned && !Interleaved ? half + V * chunk : 2 * V * chunk + V;
+    const bool in = V * chunk < half;
+    at[0] = kApart ? V * chunk : Interleaved ? 2 * chunk : in ? V * chunk : half + V * chunk;
+    at[1] = kApart ? dim / 2 + V * chunk : Interleaved ? 2 * chunk + 1 : in ? half + V * chunk : dim / 2 + V * chunk;
+    turned[0] = kApart ? at[0] < 2 * half : in;
+    turned[1] = kApart ? at[1] < 2 * half : in;
+  }
+  __device__ __forceinline__ bool turns(int i) const { return turned[kApart ? i / kOfPack : 0]; }
+  // the pair i in the tables, 0 where it is not turned
+  __device__ __forceinline__ unsigned angle(int i) const {
+    const unsigned first = Interleaved ? at[kApart ? i / kOfPack : 0] / 2 : at[0];
+    return any && turns(i) ? first + i % kOfPack : 0u;
   }
 };
 
@@ -109,21 +121,6 @@ __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p
   store_vec<T, V, Stream>(row + p.at[1], b);
 }
 
-// V elements of a row of angles from `row` on
-template <int V> __device__ __forceinline__ void load_floats(const HeadsArgs &a, const float *row, float (&x)[V]) {
-  constexpr int N = V < 4 ? V : 4;
-#pragma unroll
-  for (int i = 0; i < V; i += N) {
-    Vec<float, N> part;
-    if (a.wide_angles) part = load_vec<float, N>(row + i);
-    else
-#pragma unroll
-      for (int k = 0; k < N; ++k) part[k] = row[i + k];
-#pragma unroll
-    for (int k = 0; k < N; ++k) x[i + k] = part[k];
-  }
-}
-
 // The axes of the pairs lane, lane + 64, .. of a row, a byte each; 255: none.
 __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
   unsigned axes = ~0u;
@@ -133,54 +130,73 @@ __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
   return axes;
 }
 
-// Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  With
-// one axis a lane reads them from the one row of the token.  With several the lanes of the wave read a pair each and share them through LDS, as
-// every row of the wave needs the same (5003 tokens of 16 heads with three axes 10.9 us; 14.0 where each lane read its pairs from all rows).
-// shared: kMostDim floats of the wave.
-template <bool Axes, int V, bool Interleaved>
-__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned axes, unsigned t, float *shared, float (&c)[V], float (&s)[V]) {
+// Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  One axis: from the
+// one row of the token.
+template <int V, bool Interleaved>
+__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
   if (!a.cos_sin) return;
-  const unsigned at_lane = p.any && p.turned ? p.pair : 0u;
-  if constexpr (!Axes) {
-    const int at = a.axes ? load_scalar(a.positions + t) : -1;
-    const bool there = (unsigned)at < a.angles;
-    const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride + at_lane;
+  constexpr int kAngles = Place<V, Interleaved>::kAngles;
+  const int at = a.axes ? load_scalar(a.positions + t) : -1;
+  const bool there = (unsigned)at < a.angles;
+  const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride;
+  const float none = __builtin_nanf("");
+#pragma unroll
+  for (int i = 0; i < V; i += kAngles) {
+    Vec<float, kAngles> cosines = {}, sines = {};
     if (a.angles) {
-      load_floats(a, row, c);
-      load_floats(a, row + a.half, s);
+      const float *from = row + p.angle(i);
+      if (a.wide_angles) {
+        cosines = load_vec<float, kAngles>(from);
+        sines = load_vec<float, kAngles>(from + a.half);
+      } else
+#pragma unroll
+        for (int k = 0; k < kAngles; ++k) { cosines[k] = from[k]; sines[k] = from[a.half + k]; }
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      c[i] = there ? c[i] : __builtin_nanf("");
-      s[i] = there ? s[i] : __builtin_nanf("");
+    for (int k = 0; k < kAngles; ++k) {
+      c[i + k] = there ? cosines[k] : none;
+      s[i + k] = there ? sines[k] : none;
     }
-  } else {
+  }
+}
+
+// Several axes: the lanes of the wave read a pair each and share them through LDS, as every row of the wave needs the same (5003 tokens of 16 heads
+// with three axes 10.9 us; 14.0 where each lane read its pairs from all rows), and take them from there for each row, which frees their
+// registers.  shared: kMostDim floats of the wave.
+__device__ __forceinline__ void stage_angles(const HeadsArgs &a, unsigned axes, unsigned t, float *shared) {
+  __builtin_amdgcn_wave_barrier();                           // the lanes of a wave go together: the token before is done
 #pragma unroll
-    for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k) {
-      const unsigned n = lane_id() + kWave * k, axis = axes >> 8 * k & 255u;
-      if (n >= a.half) break;
-      const int at = axis < a.axes ? a.positions[axis * a.position_stride + t] : -1;
-      float cosine = __builtin_nanf(""), sine = cosine;
-      if ((unsigned)at < a.angles) {
-        const float *row = a.cos_sin + at * a.angle_stride + n;
-        cosine = row[0];
-        sine = row[a.half];
-      }
-      shared[n] = cosine;
-      shared[kMostDim / 2 + n] = sine;
+  for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k) {
+    const unsigned n = lane_id() + kWave * k, axis = axes >> 8 * k & 255u;
+    if (n >= a.half) break;
+    const int at = axis < a.axes ? a.positions[axis * a.position_stride + t] : -1;
+    float cosine = __builtin_nanf(""), sine = cosine;
+    if ((unsigned)at < a.angles) {
+      const float *row = a.cos_sin + at * a.angle_stride + n;
+      cosine = row[0];
+      sine = row[a.half];
     }
-    // the lanes of a wave go together, and the reads of the token before are done as their values are
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    typedef Vec<float, V> Some;
-    const Some cosines = *reinterpret_cast<const Some *>(shared + at_lane), sines = *reinterpret_cast<const Some *>(shared + kMostDim / 2 + at_lane);
+    shared[n] = cosine;
+    shared[kMostDim / 2 + n] = sine;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+template <int V, bool Interleaved> __device__ __forceinline__ void staged_angles(const Place<V, Interleaved> &p, const float *shared, float (&c)[V], float (&s)[V]) {
+  constexpr int kAngles = Place<V, Interleaved>::kAngles;
+  typedef Vec<float, kAngles> Some;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      c[i] = cosines[i];
-      s[i] = sines[i];
+  for (int i = 0; i < V; i += kAngles) {
+    unsigned at = p.angle(i);
+    asm volatile("" : "+v"(at));                             // read for each row: kept, they would take the registers that this is to free
+    const float *from = shared + at;
+    const Some cosines = *reinterpret_cast<const Some *>(from), sines = *reinterpret_cast<const Some *>(from + kMostDim / 2);
+#pragma unroll
+    for (int k = 0; k < kAngles; ++k) {
+      c[i + k] = cosines[k];
+      s[i + k] = sines[k];
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -246,7 +262,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next = load(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    load_angles<Axes>(a, p, axes, t, shared[Axes ? wave_id() : 0], c, s);
+    if constexpr (Axes) stage_angles(a, axes, t, shared[wave_id()]);
+    else load_angles(a, p, t, c, s);
     const long long slot = a.slots ? load_scalar(a.slots + t) : 0;
     const bool stored = !a.slots || (unsigned long long)slot < a.places;
     const unsigned page = a.slots && stored ? (unsigned)slot / a.page : 0u, place = a.slots && stored ? (unsigned)slot - page * a.page : 0u;
@@ -258,14 +275,15 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
       unpack(now, p, x);
       const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
       if (!n.is_v) {
+        if constexpr (Axes) staged_angles(p, shared[wave_id()], c, s);
         float w[2][V];
         unpack(either(n.is_q, wq, wk), p, w);
         const float r = (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? inverse_root(square * by_dim + a.eps) : 1.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float y0 = x[0][i] * r * w[0][i], y1 = x[1][i] * r * w[1][i];
-          x[0][i] = p.turned ? y0 * c[i] - y1 * s[i] : y0;
-          x[1][i] = p.turned ? y1 * c[i] + y0 * s[i] : y1;
+          x[0][i] = p.turns(i) ? y0 * c[i] - y1 * s[i] : y0;
+          x[1][i] = p.turns(i) ? y1 * c[i] + y0 * s[i] : y1;
         }
       }
       if (!n.live || (!n.is_q && !stored)) continue;
@@ -302,7 +320,8 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next_x = load_x(Turn(a, first + row_of_wave, end), t), next_g = load_g(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    load_angles<Axes>(a, p, axes, t, sums[wave_id()][0], c, s);
+    if constexpr (Axes) stage_angles(a, axes, t, sums[wave_id()][0]);
+    else load_angles(a, p, t, c, s);
     for (unsigned h0 = first; h0 < end; h0 += rows) {
       const Turn n(a, h0 + row_of_wave, end);
       float x[2][V], g[2][V];
@@ -311,11 +330,12 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
       const Turn then(a, h0 + rows + row_of_wave, end);
       next_x = load_x(then, t);
       next_g = load_g(then, t);
+      if constexpr (Axes) staged_angles(p, sums[wave_id()][0], c, s);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float g0 = g[0][i], g1 = g[1][i];
-        g[0][i] = p.turned ? g0 * c[i] + g1 * s[i] : g0;
-        g[1][i] = p.turned ? g1 * c[i] - g0 * s[i] : g1;
+        g[0][i] = p.turns(i) ? g0 * c[i] + g1 * s[i] : g0;
+        g[1][i] = p.turns(i) ? g1 * c[i] - g0 * s[i] : g1;
       }
       if (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
         // the sums are taken by all lanes of a row together: a row is of q or of k as a whole.  A row that no head has is zeros, whose norm
