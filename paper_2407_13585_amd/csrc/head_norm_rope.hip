@@ -52,16 +52,18 @@ template <int V, bool Interleaved> struct Place {
   static constexpr int kOfPack = kApart ? V / 2 : V;
   static constexpr int kAngles = kOfPack < 4 ? kOfPack : 4;          // angles that are read at once
   unsigned at[2];
-  bool any, turned[2];
+  bool any, turned[kApart ? V : 1]; // turned: of the pairs; a pack that has its own may hold the last turned one and the first that is not
   __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
     any = 2 * V * chunk < dim;
     const bool in = V * chunk < half;
     at[0] = kApart ? V * chunk : Interleaved ? 2 * chunk : in ? V * chunk : half + V * chunk;
     at[1] = kApart ? dim / 2 + V * chunk : Interleaved ? 2 * chunk + 1 : in ? half + V * chunk : dim / 2 + V * chunk;
-    turned[0] = kApart ? at[0] < 2 * half : in;
-    turned[1] = kApart ? at[1] < 2 * half : in;
+    if constexpr (kApart) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) turned[i] = at[i / kOfPack] / 2 + i % kOfPack < half;
+    } else turned[0] = in;
   }
-  __device__ __forceinline__ bool turns(int i) const { return turned[kApart ? i / kOfPack : 0]; }
+  __device__ __forceinline__ bool turns(int i) const { return turned[kApart ? i : 0]; }
   // the pair i in the tables, 0 where it is not turned
   __device__ __forceinline__ unsigned angle(int i) const {
     const unsigned first = Interleaved ? at[kApart ? i / kOfPack : 0] / 2 : at[0];
@@ -144,13 +146,20 @@ __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, I
   for (int i = 0; i < V; i += kAngles) {
     Vec<float, kAngles> cosines = {}, sines = {};
     if (a.angles) {
-      const float *from = row + p.angle(i);
       if (a.wide_angles) {
+        const float *from = row + p.angle(i);
         cosines = load_vec<float, kAngles>(from);
         sines = load_vec<float, kAngles>(from + a.half);
-      } else
+      } else {
+        unsigned first = p.angle(i);
+        asm volatile("" : "+v"(first));                      // what follows is not to be kept in registers from token to token
 #pragma unroll
-        for (int k = 0; k < kAngles; ++k) { cosines[k] = from[k]; sines[k] = from[a.half + k]; }
+        for (int k = 0; k < kAngles; ++k) {
+          const unsigned n = Interleaved ? min(first + k, a.half - 1) : first + k;
+          cosines[k] = row[n];
+          sines[k] = row[a.half + n];
+        }
+      }
     }
 #pragma unroll
     for (int k = 0; k < kAngles; ++k) {
@@ -249,7 +258,7 @@ template <int V> __device__ __forceinline__ float sum_of_products(const float (&
 }
 
 template <class T, int V, bool Interleaved, bool Stream, bool Axes>
-__global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
+__global__ __launch_bounds__(kThreads, Axes ? 4 : 5) void heads_kernel(HeadsArgs a) {
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
   const Place<V, Interleaved> p(a.dim, a.half, chunk);
@@ -508,17 +517,20 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
   a.eps = (float)eps;
   call.dtype = dtype;
   call.interleaved = interleaved != 0;
-  // 16 bytes a pack, less where the pairs, the strides or the alignment of an array do not allow it
+  // 16 bytes a pack, less where the pairs, the strides or the alignment of an array do not allow it (neighbours that are paired stay in one pack:
+  // the gradient of 12844 tokens of 28 heads of 72 with 18 elements turned 61 us, 157 with packs that end where the turned ones do)
   call.pack = 16 / size_of_dtype(dtype);
-  while (call.pack > 1 && (a.half % call.pack || dim / 2 % call.pack)) call.pack /= 2;
-  a.wide_angles = a.cos_sin && common_alignment(cos_sin, 4) == 4;
+  while (call.pack > 1 && ((!interleaved && a.half % call.pack) || dim / 2 % call.pack)) call.pack /= 2;
   for (const fc_tensor *t : {&q, &k, &q_weight, &k_weight})
     if (present(*t)) call.pack = common_alignment(*t, call.pack);
+  a.wide_angles = a.cos_sin && common_alignment(cos_sin, 4) == 4;
   return FC_OK;
 }
 
 // once the packs are known
 int settle_lanes(TensorChecks &c, HeadsCall &call) {
+  // angles are read as many at once as a pack has pairs, at most four
+  call.a.wide_angles = call.a.wide_angles && call.a.half % std::max(1, std::min(call.interleaved ? call.pack / 2 : call.pack, 4)) == 0;
   unsigned lanes = 1;
   while (lanes * 2 * call.pack < call.a.dim) { lanes *= 2; ++call.a.lanes_log2; }
   if (lanes > (unsigned)kWave)

@@ -308,6 +308,22 @@ def test_rotation_without_a_norm_and_positions_out_of_range(dtype, axes):
     check_heads(heads_case(31, 4, 2, 64, 48, dtype, seed=9, axes=axes, bad=True), dtype, interleaved=True)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("axes", [1, 3])
+@pytest.mark.parametrize("dim,rotary", [(72, 18), (80, 20), (112, 28), (128, 128), (256, 250), (512, 46)])
+def test_rotation_that_ends_inside_what_is_read_at_once(dtype, axes, dim, rotary):
+    s = heads_case(29, 5, 2, dim, rotary, dtype, seed=dim + axes, axes=axes)
+    check_heads(s, dtype, interleaved=True)
+    check_grad(s, dtype, interleaved=True)
+    wide = gpu(np.zeros((500, rotary + 3), np.float32))                                    # rows of angles that are not aligned
+    wide[:, 1:1 + rotary] = s["cos_sin"]
+    s["cos_sin"] = wide[:, 1:1 + rotary]
+    check_heads(s, dtype, interleaved=True)
+    if dim <= 128:
+        check_heads(s, dtype)
+        check_grad(s, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_norm_and_rotation_in_place(dtype):
     check_heads(heads_case(77, 6, 3, 96, 96, dtype, seed=2), dtype, in_place=True)
