@@ -44,29 +44,44 @@ struct HeadsArgs {
   bool wide_angles;                 // rows of cos_sin are aligned for packs
 };
 
+// Which elements are turned together, and how a lane comes by both.  kHalves: y[i] and y[i + R/2], in two packs that are R/2 apart.  kNeighbours:
+// y[2i] and y[2i+1], side by side in a pack.  kCrossed: y[i] and y[i + R/2] where R/2 is no multiple of a pack: the packs lie as those of neighbours
+// do, and the row's turned elements are exchanged through LDS.
+constexpr int kHalves = 0, kNeighbours = 1, kCrossed = 2;
+
 // Where a lane's two packs of a row lie, the same for all rows, and which pairs they hold.  The packs of neighbouring lanes lie side by side, so that
 // an instruction reads whole lines (6966 tokens of 16 heads of 256, f32, half of them turned, neighbours paired, 46 us; 55 with a lane's two packs in a row).
-template <int V, bool Interleaved> struct Place {
+template <int V, int Pairs> struct Place {
   // the i-th pair is of pack i / kOfPack; one element a pack is half a pair
-  static constexpr bool kApart = Interleaved && V > 1;               // the packs have pairs of their own
-  static constexpr int kOfPack = kApart ? V / 2 : V;
+  static constexpr bool kOwn = Pairs == kNeighbours && V > 1;        // the packs have pairs of their own
+  static constexpr int kOfPack = kOwn ? V / 2 : V;
   static constexpr int kAngles = kOfPack < 4 ? kOfPack : 4;          // angles that are read at once
   unsigned at[2];
-  bool any, turned[kApart ? V : 1]; // turned: of the pairs; a pack that has its own may hold the last turned one and the first that is not
+  // turned: of the pairs, which are those of both packs (kHalves), of one or the other (kOwn; a pack may hold the last turned one and the first that
+  // is not), or of the elements (kCrossed)
+  bool any, turned[Pairs == kCrossed ? 2 * V : kOwn ? V : 1];
   __device__ __forceinline__ Place(unsigned dim, unsigned half, unsigned chunk) {
     any = 2 * V * chunk < dim;
     const bool in = V * chunk < half;
-    at[0] = kApart ? V * chunk : Interleaved ? 2 * chunk : in ? V * chunk : half + V * chunk;
-    at[1] = kApart ? dim / 2 + V * chunk : Interleaved ? 2 * chunk + 1 : in ? half + V * chunk : dim / 2 + V * chunk;
-    if constexpr (kApart) {
+    if constexpr (Pairs == kCrossed || kOwn) {
+      at[0] = V * chunk;
+      at[1] = dim / 2 + V * chunk;
+    } else {
+      at[0] = Pairs == kNeighbours ? 2 * chunk : in ? V * chunk : half + V * chunk;
+      at[1] = Pairs == kNeighbours ? 2 * chunk + 1 : in ? half + V * chunk : dim / 2 + V * chunk;
+    }
+    if constexpr (Pairs == kCrossed) {
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) turned[i] = any && at[i / V] + i % V < 2 * half;
+    } else if constexpr (kOwn) {
 #pragma unroll
       for (int i = 0; i < V; ++i) turned[i] = at[i / kOfPack] / 2 + i % kOfPack < half;
     } else turned[0] = in;
   }
-  __device__ __forceinline__ bool turns(int i) const { return turned[kApart ? i : 0]; }
+  __device__ __forceinline__ bool turns(int i) const { return turned[kOwn ? i : 0]; }
   // the pair i in the tables, 0 where it is not turned
   __device__ __forceinline__ unsigned angle(int i) const {
-    const unsigned first = Interleaved ? at[kApart ? i / kOfPack : 0] / 2 : at[0];
+    const unsigned first = Pairs == kNeighbours ? at[kOwn ? i / kOfPack : 0] / 2 : at[0];
     return any && turns(i) ? first + i % kOfPack : 0u;
   }
 };
@@ -77,8 +92,8 @@ template <class T, int V> struct Packs {
 };
 
 // zeros where there is nothing, or where `live` is false
-template <bool Stream, class T, int V, bool Interleaved>
-__device__ __forceinline__ Packs<T, V> load_packs(const T *row, const Place<V, Interleaved> &p, bool live) {
+template <bool Stream, class T, int V, int Pairs>
+__device__ __forceinline__ Packs<T, V> load_packs(const T *row, const Place<V, Pairs> &p, bool live) {
   Packs<T, V> x;
 #pragma unroll
   for (int i = 0; i < V; ++i) x.a[i] = x.b[i] = (T)0.0f;
@@ -90,10 +105,10 @@ __device__ __forceinline__ Packs<T, V> load_packs(const T *row, const Place<V, I
 }
 
 // its pairs: the i-th is (x[0][i], x[1][i])
-template <class T, int V, bool Interleaved> __device__ __forceinline__ void unpack(const Packs<T, V> &w, const Place<V, Interleaved> &, float (&x)[2][V]) {
+template <class T, int V, int Pairs> __device__ __forceinline__ void unpack(const Packs<T, V> &w, const Place<V, Pairs> &, float (&x)[2][V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if constexpr (Interleaved) {    // also behind the rotated part: the two packs follow each other there
+    if constexpr (Pairs == kNeighbours) {    // also behind the rotated part: the two packs follow each other there
       const int e = 2 * i, o = 2 * i + 1;
       x[0][i] = e < V ? (float)w.a[e % V] : (float)w.b[e % V];
       x[1][i] = o < V ? (float)w.a[o % V] : (float)w.b[o % V];
@@ -104,13 +119,13 @@ template <class T, int V, bool Interleaved> __device__ __forceinline__ void unpa
   }
 }
 
-template <bool Stream, class T, int V, bool Interleaved>
-__device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p, const float (&x)[2][V]) {
+template <bool Stream, class T, int V, int Pairs>
+__device__ __forceinline__ void store_row(T *row, const Place<V, Pairs> &p, const float (&x)[2][V]) {
   if (!p.any) return;
   Vec<T, V> a, b;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if constexpr (Interleaved) {
+    if constexpr (Pairs == kNeighbours) {
       const int e = 2 * i, o = 2 * i + 1;
       if (e < V) a[e % V] = (T)x[0][i]; else b[e % V] = (T)x[0][i];
       if (o < V) a[o % V] = (T)x[1][i]; else b[o % V] = (T)x[1][i];
@@ -125,6 +140,7 @@ __device__ __forceinline__ void store_row(T *row, const Place<V, Interleaved> &p
 
 // The axes of the pairs lane, lane + 64, .. of a row, a byte each; 255: none.
 __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
+  if (!a.axis_of) return 0u;
   unsigned axes = ~0u;
 #pragma unroll
   for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k)
@@ -134,10 +150,10 @@ __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
 
 // Cosines and sines of the pairs of this lane at token t, not used where nothing is turned: NaN where the tables have no row.  One axis: from the
 // one row of the token.
-template <int V, bool Interleaved>
-__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Interleaved> &p, unsigned t, float (&c)[V], float (&s)[V]) {
+template <int V, int Pairs>
+__device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Pairs> &p, unsigned t, float (&c)[V], float (&s)[V]) {
   if (!a.cos_sin) return;
-  constexpr int kAngles = Place<V, Interleaved>::kAngles;
+  constexpr int kAngles = Place<V, Pairs>::kAngles;
   const int at = a.axes ? load_scalar(a.positions + t) : -1;
   const bool there = (unsigned)at < a.angles;
   const float *row = a.cos_sin + (there ? at : 0) * a.angle_stride;
@@ -155,7 +171,7 @@ __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, I
         asm volatile("" : "+v"(first));                      // what follows is not to be kept in registers from token to token
 #pragma unroll
         for (int k = 0; k < kAngles; ++k) {
-          const unsigned n = Interleaved ? min(first + k, a.half - 1) : first + k;
+          const unsigned n = Pairs == kNeighbours ? min(first + k, a.half - 1) : first + k;
           cosines[k] = row[n];
           sines[k] = row[a.half + n];
         }
@@ -171,8 +187,8 @@ __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, I
 
 // Several axes: the lanes of the wave read a pair each and share them through LDS, as every row of the wave needs the same (5003 tokens of 16 heads
 // with three axes 10.9 us; 14.0 where each lane read its pairs from all rows), and take them from there for each row, which frees their
-// registers.  shared: kMostDim floats of the wave.
-__device__ __forceinline__ void stage_angles(const HeadsArgs &a, unsigned axes, unsigned t, float *shared) {
+// registers.  shared: kMostDim floats of the wave; kCrossed, where they are put down for each element, the sines with their sign: twice as many.
+template <int Pairs> __device__ __forceinline__ void stage_angles(const HeadsArgs &a, unsigned axes, unsigned t, float *shared) {
   __builtin_amdgcn_wave_barrier();                           // the lanes of a wave go together: the token before is done
 #pragma unroll
   for (unsigned k = 0; k < kMostDim / 2 / kWave; ++k) {
@@ -186,14 +202,18 @@ __device__ __forceinline__ void stage_angles(const HeadsArgs &a, unsigned axes, 
       sine = row[a.half];
     }
     shared[n] = cosine;
-    shared[kMostDim / 2 + n] = sine;
+    if constexpr (Pairs == kCrossed) {
+      shared[a.half + n] = cosine;
+      shared[kMostDim + n] = -sine;
+      shared[kMostDim + a.half + n] = sine;
+    } else shared[kMostDim / 2 + n] = sine;
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-template <int V, bool Interleaved> __device__ __forceinline__ void staged_angles(const Place<V, Interleaved> &p, const float *shared, float (&c)[V], float (&s)[V]) {
-  constexpr int kAngles = Place<V, Interleaved>::kAngles;
+template <int V, int Pairs> __device__ __forceinline__ void staged_angles(const Place<V, Pairs> &p, const float *shared, float (&c)[V], float (&s)[V]) {
+  constexpr int kAngles = Place<V, Pairs>::kAngles;
   typedef Vec<float, kAngles> Some;
 #pragma unroll
   for (int i = 0; i < V; i += kAngles) {
@@ -207,6 +227,42 @@ template <int V, bool Interleaved> __device__ __forceinline__ void staged_angles
       s[i + k] = sines[k];
     }
   }
+}
+
+// kCrossed: y turned by the staged angles, or back (Back).  lds: the row's 2 V floats a lane, where every turned element is put down in its
+// partner's place.
+template <bool Back, int V> __device__ __forceinline__ void turn_crossed(const Place<V, kCrossed> &p, unsigned half, const float *shared, float *lds, float (&y)[2][V]) {
+  constexpr int N = V < 4 ? V : 4;
+  typedef Vec<float, N> Some;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (!p.turned[k * V]) continue;
+    unsigned at = p.at[k];
+    asm volatile("" : "+v"(at));                             // places are not to be kept in registers
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (p.turned[k * V + i]) lds[at + i < half ? at + i + half : at + i - half] = y[k][i];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (!p.turned[k * V]) continue;
+    unsigned at = p.at[k];
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int i = 0; i < V; i += N) {
+      const Some other = *reinterpret_cast<const Some *>(lds + at + i), cosines = *reinterpret_cast<const Some *>(shared + at + i),
+                 sines = *reinterpret_cast<const Some *>(shared + kMostDim + at + i);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float turned = y[k][i + e] * cosines[e] + other[e] * (Back ? -sines[e] : sines[e]);
+        y[k][i + e] = p.turned[k * V + i + e] ? turned : y[k][i + e];
+      }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();                           // the next row is put down after this one is read
 }
 
 // by value: a choice between two places would put both into memory
@@ -224,7 +280,7 @@ template <class T> __device__ __forceinline__ T *row_of(Rows rows, unsigned t, u
 }
 
 // ones where there is no weight
-template <class T, int V, bool Interleaved> __device__ __forceinline__ Packs<T, V> load_weight(const void *weight, const Place<V, Interleaved> &p) {
+template <class T, int V, int Pairs> __device__ __forceinline__ Packs<T, V> load_weight(const void *weight, const Place<V, Pairs> &p) {
   Packs<T, V> w = load_packs<false>(static_cast<const T *>(weight), p, weight != nullptr);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -257,21 +313,23 @@ template <int V> __device__ __forceinline__ float sum_of_products(const float (&
   return s;
 }
 
-template <class T, int V, bool Interleaved, bool Stream, bool Axes>
+template <class T, int V, int Pairs, bool Stream, bool Axes>
 __global__ __launch_bounds__(kThreads, Axes ? 4 : 5) void heads_kernel(HeadsArgs a) {
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk);
-  const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
+  const Place<V, Pairs> p(a.dim, a.half, chunk);
+  const auto wq = load_weight<T, V, Pairs>(a.weight[0], p), wk = load_weight<T, V, Pairs>(a.weight[1], p);
   const unsigned first = blockIdx.y * a.per_wave, end = min(first + a.per_wave, a.heads[0] + a.heads[1] + a.heads[2]);
   const float by_dim = 1.0f / (float)a.dim;
   const unsigned axes = Axes ? axes_of_lane(a) : 0u;
-  __shared__ alignas(32) float shared[Axes ? kWaves : 1][Axes ? kMostDim : 1];
+  constexpr bool kCross = Pairs == kCrossed;
+  __shared__ alignas(32) float shared[Axes ? kWaves : 1][kCross ? 2 * kMostDim : Axes ? kMostDim : 1];
+  __shared__ alignas(32) float crossed[kCross ? kThreads * 2 * V : 1];
   auto load = [&](const Turn &n, unsigned t) { return load_packs<Stream>(row_of<const T>(either(n.is_q, a.q, either(n.is_v, a.v, a.k)), t, n.head), p, n.live); };
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next = load(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    if constexpr (Axes) stage_angles(a, axes, t, shared[wave_id()]);
+    if constexpr (Axes) stage_angles<Pairs>(a, axes, t, shared[wave_id()]);
     else load_angles(a, p, t, c, s);
     const long long slot = a.slots ? load_scalar(a.slots + t) : 0;
     const bool stored = !a.slots || (unsigned long long)slot < a.places;
@@ -284,16 +342,17 @@ __global__ __launch_bounds__(kThreads, Axes ? 4 : 5) void heads_kernel(HeadsArgs
       unpack(now, p, x);
       const float square = lanes_sum(sum_of_products(x, x), (int)a.lanes_log2);
       if (!n.is_v) {
-        if constexpr (Axes) staged_angles(p, shared[wave_id()], c, s);
+        if constexpr (Axes && !kCross) staged_angles(p, shared[wave_id()], c, s);
         float w[2][V];
         unpack(either(n.is_q, wq, wk), p, w);
         const float r = (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) ? inverse_root(square * by_dim + a.eps) : 1.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float y0 = x[0][i] * r * w[0][i], y1 = x[1][i] * r * w[1][i];
-          x[0][i] = p.turns(i) ? y0 * c[i] - y1 * s[i] : y0;
-          x[1][i] = p.turns(i) ? y1 * c[i] + y0 * s[i] : y1;
+          x[0][i] = !kCross && p.turns(i) ? y0 * c[i] - y1 * s[i] : y0;
+          x[1][i] = !kCross && p.turns(i) ? y1 * c[i] + y0 * s[i] : y1;
         }
+        if constexpr (kCross) turn_crossed<false>(p, a.half, shared[wave_id()], crossed + (threadIdx.x - chunk) * 2 * V, x);
       }
       if (!n.live || (!n.is_q && !stored)) continue;
       T *to;
@@ -311,13 +370,15 @@ struct GradRows {
 };
 
 // dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
-template <class T, int V, bool Interleaved, bool Stream, bool Axes>
+template <class T, int V, int Pairs, bool Stream, bool Axes>
 __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
-  __shared__ alignas(32) float sums[kWaves][2][kMostDim];
+  constexpr bool kCross = Pairs == kCrossed;
+  __shared__ alignas(32) float sums[kWaves][2][kMostDim];    // of the weights' gradients, at the end; before it the staged angles
+  __shared__ alignas(32) float crossed[kCross ? kThreads * 2 * V : 1];
   const unsigned lanes = 1u << a.lanes_log2, rows = kWave >> a.lanes_log2;
   const unsigned chunk = lane_id() & (lanes - 1), row_of_wave = lane_id() >> a.lanes_log2;
-  const Place<V, Interleaved> p(a.dim, a.half, chunk);
-  const auto wq = load_weight<T, V, Interleaved>(a.weight[0], p), wk = load_weight<T, V, Interleaved>(a.weight[1], p);
+  const Place<V, Pairs> p(a.dim, a.half, chunk);
+  const auto wq = load_weight<T, V, Pairs>(a.weight[0], p), wk = load_weight<T, V, Pairs>(a.weight[1], p);
   float dq[2][V], dk[2][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) dq[0][i] = dq[1][i] = dk[0][i] = dk[1][i] = 0.0f;
@@ -329,7 +390,7 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
   for (unsigned t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(wave_id()); t < a.tokens; t += gridDim.x * kWaves) {
     auto next_x = load_x(Turn(a, first + row_of_wave, end), t), next_g = load_g(Turn(a, first + row_of_wave, end), t);
     float c[V] = {}, s[V] = {};
-    if constexpr (Axes) stage_angles(a, axes, t, sums[wave_id()][0]);
+    if constexpr (Axes) stage_angles<Pairs>(a, axes, t, sums[wave_id()][0]);
     else load_angles(a, p, t, c, s);
     for (unsigned h0 = first; h0 < end; h0 += rows) {
       const Turn n(a, h0 + row_of_wave, end);
@@ -339,12 +400,15 @@ __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, Gr
       const Turn then(a, h0 + rows + row_of_wave, end);
       next_x = load_x(then, t);
       next_g = load_g(then, t);
-      if constexpr (Axes) staged_angles(p, sums[wave_id()][0], c, s);
+      if constexpr (kCross) turn_crossed<true>(p, a.half, sums[wave_id()][0], crossed + (threadIdx.x - chunk) * 2 * V, g);
+      else {
+        if constexpr (Axes) staged_angles(p, sums[wave_id()][0], c, s);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float g0 = g[0][i], g1 = g[1][i];
-        g[0][i] = p.turns(i) ? g0 * c[i] + g1 * s[i] : g0;
-        g[1][i] = p.turns(i) ? g1 * c[i] - g0 * s[i] : g1;
+        for (int i = 0; i < V; ++i) {
+          const float g0 = g[0][i], g1 = g[1][i];
+          g[0][i] = p.turns(i) ? g0 * c[i] + g1 * s[i] : g0;
+          g[1][i] = p.turns(i) ? g1 * c[i] - g0 * s[i] : g1;
+        }
       }
       if (n.is_q ? a.weight[0] != nullptr : a.weight[1] != nullptr) {
         // the sums are taken by all lanes of a row together: a row is of q or of k as a whole.  A row that no head has is zeros, whose norm
@@ -427,9 +491,11 @@ __global__ __launch_bounds__(1024) void weight_grad_kernel(const float *partial,
 
 // ------------------------------------------------------------------ host
 // calls f with the type, the elements of a pack, the pairing and the way through the caches of this call as compile-time values
-template <class F> void with_form(int32_t dtype, int pack, bool interleaved, bool stream, bool axes, F &&f) {
+template <class F> void with_form(int32_t dtype, int pack, int pairs, bool stream, bool axes, F &&f) {
   auto by_axes = [&](auto element, auto v, auto paired, auto past) {
-    axes ? f(element, v, paired, past, std::true_type{}) : f(element, v, paired, past, std::false_type{});
+    if constexpr (decltype(paired)::value == kCrossed) {
+      if constexpr (decltype(v)::value > 1) f(element, v, paired, past, std::true_type{});
+    } else axes ? f(element, v, paired, past, std::true_type{}) : f(element, v, paired, past, std::false_type{});
   };
   auto by_pack = [&](auto element, auto paired) {
     using T = decltype(element);
@@ -440,7 +506,11 @@ template <class F> void with_form(int32_t dtype, int pack, bool interleaved, boo
     else if (pack == 2) by_axes(element, std::integral_constant<int, 2>{}, paired, std::false_type{});
     else by_axes(element, std::integral_constant<int, 1>{}, paired, std::false_type{});
   };
-  auto by_pairing = [&](auto element) { interleaved ? by_pack(element, std::true_type{}) : by_pack(element, std::false_type{}); };
+  auto by_pairing = [&](auto element) {
+    if (pairs == kNeighbours) by_pack(element, std::integral_constant<int, kNeighbours>{});
+    else if (pairs == kCrossed) by_pack(element, std::integral_constant<int, kCrossed>{});
+    else by_pack(element, std::integral_constant<int, kHalves>{});
+  };
   if (dtype == FC_F32) by_pairing(float{});
   else if (dtype == FC_F16) by_pairing(_Float16{});
   else by_pairing(__bf16{});
@@ -452,7 +522,7 @@ struct HeadsCall {
   HeadsArgs a{};
   int32_t dtype;
   int pack;
-  bool interleaved;
+  int pairs;
   dim3 grid;
   unsigned heads() const { return a.heads[0] + a.heads[1] + a.heads[2]; }
   // What is read and written passes the caches where they would not hold it until it is used (16384 tokens of 40 heads 70 us through them,
@@ -516,11 +586,10 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
   a.dim = (unsigned)dim;
   a.eps = (float)eps;
   call.dtype = dtype;
-  call.interleaved = interleaved != 0;
-  // 16 bytes a pack, less where the pairs, the strides or the alignment of an array do not allow it (neighbours that are paired stay in one pack:
-  // the gradient of 12844 tokens of 28 heads of 72 with 18 elements turned 61 us, 157 with packs that end where the turned ones do)
+  call.pairs = interleaved ? kNeighbours : kHalves;
+  // 16 bytes a pack, less where the elements of a head, the strides or the alignment of an array do not allow it
   call.pack = 16 / size_of_dtype(dtype);
-  while (call.pack > 1 && ((!interleaved && a.half % call.pack) || dim / 2 % call.pack)) call.pack /= 2;
+  while (call.pack > 1 && dim / 2 % call.pack) call.pack /= 2;
   for (const fc_tensor *t : {&q, &k, &q_weight, &k_weight})
     if (present(*t)) call.pack = common_alignment(*t, call.pack);
   a.wide_angles = a.cos_sin && common_alignment(cos_sin, 4) == 4;
@@ -529,19 +598,27 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
 
 // once the packs are known
 int settle_lanes(TensorChecks &c, HeadsCall &call) {
-  // angles are read as many at once as a pack has pairs, at most four
-  call.a.wide_angles = call.a.wide_angles && call.a.half % std::max(1, std::min(call.interleaved ? call.pack / 2 : call.pack, 4)) == 0;
+  // Packs of halves end where the rotated part does, unless that leaves one or two elements: larger ones that cross take the gradient of 12844 tokens of
+  // 28 heads of 72 with 18 elements turned in 66 us, packs of one in 129; with 20 of 80 69, packs of two 97; but with 40 of 80 69, packs of four 54.
+  // Neighbours stay in one pack either way (60 us, 157 with packs that end there too).
+  int pack = call.pack;
+  while (call.pairs == kHalves && pack > 1 && call.a.half % pack) pack /= 2;
   unsigned lanes = 1;
-  while (lanes * 2 * call.pack < call.a.dim) { lanes *= 2; ++call.a.lanes_log2; }
+  while (lanes * 2 * pack < call.a.dim) lanes *= 2;
   if (lanes > (unsigned)kWave)
-    return c.fail(FC_E_UNSUPPORTED, "heads of " + std::to_string(call.a.dim) + " elements can be read " + std::to_string(call.pack) +
-                                        " at a time only (rotated pairs, strides and alignment): at most " + std::to_string(128 * call.pack) + " are built for").code();
+    return c.fail(FC_E_UNSUPPORTED, "heads of " + std::to_string(call.a.dim) + " elements can be read " + std::to_string(pack) +
+                                        " at a time only (rotated pairs, strides and alignment): at most " + std::to_string(128 * pack) + " are built for").code();
+  if (pack < call.pack && pack <= 2) call.pairs = kCrossed;
+  else call.pack = pack;
+  while ((2u * call.pack << call.a.lanes_log2) < call.a.dim) ++call.a.lanes_log2;
+  // angles are read as many at once as a pack has pairs, at most four
+  call.a.wide_angles = call.a.wide_angles && call.a.half % std::max(1, std::min(call.pairs == kNeighbours ? call.pack / 2 : call.pack, 4)) == 0;
   return FC_OK;
 }
 
 struct HeadNormRope final : Operator, HeadsCall {
   template <class F> void with_kernel(F &&f) const {
-    with_form(dtype, pack, interleaved, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
+    with_form(dtype, pack, pairs, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
       f(&heads_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value, decltype(axes)::value>);
     });
   }
@@ -558,7 +635,7 @@ struct HeadNormRopeGrad final : Operator, HeadsCall {
   unsigned groups() const { return grid.x * grid.y; }
   size_t workspace() const override { return dw[0] || dw[1] ? (size_t)groups() * 2 * a.dim * sizeof(float) : 0; }
   template <class F> void with_kernel(F &&f) const {
-    with_form(dtype, pack, interleaved, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
+    with_form(dtype, pack, pairs, stream(), a.axis_of != nullptr, [&](auto element, auto v, auto paired, auto past, auto axes) {
       f(&heads_grad_kernel<decltype(element), decltype(v)::value, decltype(paired)::value, decltype(past)::value, decltype(axes)::value>);
     });
   }

@@ -324,6 +324,19 @@ def test_rotation_that_ends_inside_what_is_read_at_once(dtype, axes, dim, rotary
         check_grad(s, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("axes", [1, 3])
+def test_halves_that_do_not_lie_a_whole_read_apart(dtype, axes):
+    for dim, rotary in [(72, 18), (80, 20), (112, 28), (72, 36)]:
+        slots = np.random.default_rng(dim).permutation(80)[:37].astype(np.int64)
+        slots[::6] = -1
+        check_heads(heads_case(37, 19, 6, dim, rotary, dtype, seed=dim, axes=axes), dtype, slots=slots, page=8, pages=10)
+        check_heads(heads_case(37, 19, 6, dim, rotary, dtype, seed=dim, axes=axes, bad=True), dtype)
+        check_heads(heads_case(300, 3, 2, dim, rotary, dtype, seed=dim, axes=axes), dtype, weight=False, in_place=True)
+        check_grad(heads_case(700, 9, 2, dim, rotary, dtype, seed=dim, axes=axes), dtype)
+        check_grad(heads_case(5, 40, 8, dim, rotary, dtype, seed=dim, axes=axes), dtype, weight=False, in_place=True)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_norm_and_rotation_in_place(dtype):
     check_heads(heads_case(77, 6, 3, 96, 96, dtype, seed=2), dtype, in_place=True)
