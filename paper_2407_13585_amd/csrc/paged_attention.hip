@@ -20,7 +20,7 @@
 //
 // Reading the cache once bounds it where that is long, the launch and a chain of reads (lengths, page, keys, pieces) where it is not:
 //   one request of 131072 keys, 8 key heads of 128, 64 heads (bf16, 537 MB) 88 us, 6.1 TB/s; 64 requests of 1 to 8192 keys, 8 key heads of 128 (bf16)
-//   169 us, 6.3 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB) 33 us, 3.4 TB/s, where the six
+//   169 us, 6.3 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB) 31.5 us, 3.5 TB/s, where the six
 //   units of a workgroup are too few to hide its start and end; 4 requests of up to 300 keys, 2 key heads of 64 (f16) 7.0 us.
 #include "operators.hpp"
 
