@@ -161,7 +161,7 @@ template <class T> __device__ __forceinline__ Share share_of(const AttentionArgs
   before += upto - mine;
   if (s.at >= before && s.at < before + mine) {
     unsigned b = b0;
-    for (;; ++b) {
+    for (; b + 1 < b1; ++b) {
       const unsigned here = span_of<T>(a, a.lengths[b]).units * rows;
       if (s.at < before + here) break;
       before += here;
@@ -797,9 +797,14 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   }
   a.scale = (float)n.scale;
   a.wide_out = common_alignment(n.out, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) == 16;
-  const int64_t units = ceil_div((uint64_t)a.width * a.page, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;      // of a request: one more where a window starts inside
-  if (units * requests * kv * a.tiles > 0x7fffffff) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
-  op->most_units = (unsigned)(units * requests * kv * a.tiles);
+  // of a request, whose length is below 2^31 whatever its table could hold: one more where a window starts inside
+  const uint64_t keys = std::min<uint64_t>((uint64_t)a.width * a.page, 0x7fffffffu);
+  const unsigned units = ceil_div(keys, dtype == FC_F32 ? kUnit<float> : kUnit<_Float16>) + 1;
+  unsigned most_units;
+  if (__builtin_mul_overflow(units, a.requests, &most_units) || __builtin_mul_overflow(most_units, a.kv_heads, &most_units) ||
+      __builtin_mul_overflow(most_units, a.tiles, &most_units) || most_units > 0x7fffffffu)
+    return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
+  op->most_units = most_units;
   op->settle_workers();
   out = std::move(op);
   return FC_OK;

@@ -1,0 +1,40 @@
+"""Extents of the operators of a serving cache that their kernels cannot count: refused before anything is enqueued, and what lies just
+below them taken.  No GPU: the arrays are addresses that nothing reads."""
+import pytest
+
+import paper_2407_13585_amd as fc
+from test_operators import SCRATCH, T, attention
+
+
+def expect(code, *ops):
+    for call in (lambda: fc.fc_operators_scratch_bytes(ops), lambda: fc.fc_run_operators(ops, SCRATCH), lambda: fc.BoundOperators(ops, SCRATCH)):
+        with pytest.raises(fc.FcError) as e:
+            call()
+        assert e.value.name == code, str(e.value)
+
+
+def taken(*ops):
+    fc.fc_operators_scratch_bytes(ops)
+    fc.BoundOperators(ops, SCRATCH)
+
+
+def attention_over(width, page, requests, kv=2, group=2, dtype="bfloat16"):
+    cache = T(dtype, 9, page, kv, 64)
+    return attention(q=T(dtype, requests, kv * group, 64), out=T(dtype, requests, kv * group, 64), lse=None, lengths=T("int32", requests),
+                     table=T("int32", requests, width, stride=(0, 1)), k_cache=cache, v_cache=cache)
+
+
+@pytest.mark.parametrize("width", [1 << 22, 1 << 23, (1 << 23) + 1, 1 << 24, (1 << 31) - 1])
+def test_attention_counts_the_keys_of_wide_tables_in_full(width):
+    # 2^22 pages of 65536 places are 2^38 places, 2^23 are 2^32 pieces of 128: a request has up to 2^31-1 keys of them, 2^24 pieces
+    expect("FC_E_LIMIT", attention_over(width, 65536, requests=300))
+    expect("FC_E_LIMIT", attention_over(width, 65536, requests=64, kv=2))
+    taken(attention_over(width, 65536, requests=63, kv=2))
+
+
+def test_attention_counts_requests_and_heads_in_full():
+    expect("FC_E_LIMIT", attention_over(0, 16, requests=1 << 30, kv=2))                   # 2^31
+    expect("FC_E_LIMIT", attention_over((1 << 31) - 1, (1 << 31) - 1, requests=1 << 20, kv=1 << 20))     # 2^64
+    expect("FC_E_LIMIT", attention_over(8, 16, requests=1 << 16, kv=1 << 16))             # 2^33
+    taken(attention_over(0, 16, requests=(1 << 30) - 1, kv=2))
+    taken(attention_over(8, 16, requests=1 << 15, kv=1 << 14))
