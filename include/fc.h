@@ -369,7 +369,7 @@ typedef struct fc_page_map {
  * In 32 bits, rounded once.  Keys go to k_out, or, with values as they are, to row slots[t] of the caches (page slots[t] / P, place
  * slots[t] mod P); slots outside the cache, -1 among them, are skipped; slots of one call are distinct.  A position or an axis outside
  * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides).
- * At most 255 axes and 2^31-1 places of the cache (FC_E_LIMIT).  Rows are read 16 bytes at a time; where D/2, R/2 (not interleaved), a stride
+ * At most 255 axes, 2^31-1 places of the cache and 2^31-1 heads of a token, all of q, k and (with slots) v (FC_E_LIMIT).  Rows are read 16 bytes at a time; where D/2, R/2 (not interleaved), a stride
  * or an alignment does not allow it fewer, and then D is at most 128 times the elements of a read (FC_E_UNSUPPORTED). */
 typedef struct fc_head_norm_rope {
   fc_tensor q;            /* [T, Hq, D]: f32, f16 or bf16; D even, at most 512 */

@@ -543,7 +543,7 @@ struct HeadsCall {
 
 // what the operator and its gradient have in common
 int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const fc_tensor &q_weight, const fc_tensor &k_weight, const fc_tensor &cos_sin,
-                const fc_tensor &positions, const fc_tensor &axis_of, double eps, int32_t interleaved, HeadsCall &call) {
+                const fc_tensor &positions, const fc_tensor &axis_of, double eps, int32_t interleaved, bool values, HeadsCall &call) {
   const int32_t dtype = q.dtype;
   if (dtype != FC_F32 && dtype != FC_F16 && dtype != FC_BF16) return c.fail(FC_E_ARG, "q: type f32, f16 or bf16 is needed").code();
   c.array("q", q, dtype, {-1, -1, -1});
@@ -563,7 +563,8 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
   }
   if (c.ok() && !(eps >= 0 && std::isfinite((float)eps))) c.fail(FC_E_ARG, "eps must be finite, in 32 bits too, and not negative");
   if (c.ok() && (dim < 2 || dim % 2 || dim > (int64_t)kMostDim)) c.fail(FC_E_UNSUPPORTED, "heads have an even number of elements, at most 512");
-  if (c.ok() && tokens * (q.shape[1] + k.shape[1]) > (int64_t)1 << 40) c.fail(FC_E_LIMIT, "too many heads");
+  // a token's heads, those of values among them, are numbered in one row, which a wave walks in steps of up to 64 that must not pass 32 bits
+  if (c.ok() && (q.shape[1] + (values ? 2 : 1) * k.shape[1] > 0x7fffffff || tokens * (q.shape[1] + k.shape[1]) > (int64_t)1 << 40)) c.fail(FC_E_LIMIT, "too many heads");
   if (!c.ok()) return c.code();
   HeadsArgs &a = call.a;
   a.q = rows_at(q);
@@ -653,7 +654,7 @@ struct HeadNormRopeGrad final : Operator, HeadsCall {
 int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &out, std::string &err) {
   TensorChecks c(err);
   auto op = std::make_unique<HeadNormRope>();
-  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, *op) != FC_OK) return c.code();
+  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, present(n.slots), *op) != FC_OK) return c.code();
   HeadsArgs &a = op->a;
   const int64_t tokens = a.tokens, dim = a.dim, kv = a.heads[1];
   c.array("q_out", n.q_out, op->dtype, {tokens, a.heads[0], dim}, true);
@@ -698,7 +699,7 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
 int make_head_norm_rope_grad(const fc_head_norm_rope_grad &n, std::unique_ptr<Operator> &out, std::string &err) {
   TensorChecks c(err);
   auto op = std::make_unique<HeadNormRopeGrad>();
-  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, *op) != FC_OK) return c.code();
+  if (check_heads(c, n.q, n.k, n.q_weight, n.k_weight, n.cos_sin, n.positions, n.axis_of, n.eps, n.interleaved, false, *op) != FC_OK) return c.code();
   HeadsArgs &a = op->a;
   const int64_t tokens = a.tokens, dim = a.dim;
   c.array("dq_out", n.dq_out, op->dtype, {tokens, a.heads[0], dim});

@@ -3,7 +3,7 @@ below them taken.  No GPU: the arrays are addresses that nothing reads."""
 import pytest
 
 import paper_2407_13585_amd as fc
-from test_operators import SCRATCH, T, attention
+from test_operators import SCRATCH, T, attention, heads, into_cache
 
 
 def expect(code, *ops):
@@ -38,3 +38,26 @@ def test_attention_counts_requests_and_heads_in_full():
     expect("FC_E_LIMIT", attention_over(8, 16, requests=1 << 16, kv=1 << 16))             # 2^33
     taken(attention_over(0, 16, requests=(1 << 30) - 1, kv=2))
     taken(attention_over(8, 16, requests=1 << 15, kv=1 << 14))
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_heads_of_a_token_are_counted_in_full(grad):
+    def of(hq, hk):
+        q, k = (T("bfloat16", 1, h, 2) for h in (hq, hk))
+        outs = dict(dq_out=q, dk_out=k, dq=q, dk=k, dq_weight=None, dk_weight=None) if grad else dict(q_out=q, k_out=k)
+        return heads(grad, dim=2, tokens=1, q=q, k=k, q_weight=None, k_weight=None, **outs)
+    most = (1 << 31) - 1
+    for hq, hk in ((most, most), (1 << 30, 1 << 30), (most, 1), (1, most)):
+        expect("FC_E_LIMIT", of(hq, hk))
+    for hq, hk in ((most, 0), (most - 1, 1), (1, most - 1)):
+        taken(of(hq, hk))
+
+
+def test_heads_that_go_into_the_cache_are_counted_in_full():
+    def of(hq, hk):
+        none = T("bfloat16", 0, 16, hk, 2, ptr=0)
+        q, k = (T("bfloat16", 1, h, 2) for h in (hq, hk))
+        return into_cache(q=q, k=k, v=k, q_out=q, q_weight=None, k_weight=None, cos_sin=None, positions=None, k_cache=none, v_cache=none, slots=T("int64", 1))
+    expect("FC_E_LIMIT", of(2, (1 << 30) - 1))
+    expect("FC_E_LIMIT", of((1 << 31) - 1, (1 << 31) - 1))
+    taken(of(1, (1 << 30) - 1))
