@@ -409,8 +409,8 @@ typedef struct fc_head_norm_rope_grad {
  * outside the cache or the table are not there.  Query head h reads key head h / (Hq / Hk).
  *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
  * A request without keys gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key head, of as many keys as its
- * table could hold, 2^31-1 at most) are counted in 31 bits (FC_E_LIMIT).  What lies in the pages past a request's length is not looked at,
- * whatever it holds. */
+ * table could hold, 2^31-1 at most) are counted in 31 bits, the elements of a request's heads, four at a time, too (FC_E_LIMIT).  What lies
+ * in the pages past a request's length is not looked at, whatever it holds. */
 typedef struct fc_paged_attention {
   fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
   fc_tensor k_cache;      /* [pages, P, Hk, D], in any order of strides with D innermost; rows 16-byte aligned */

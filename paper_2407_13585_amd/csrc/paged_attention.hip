@@ -756,6 +756,8 @@ int make_paged_attention(const fc_paged_attention &n, std::unique_ptr<Operator> 
   for (const fc_tensor *t : {&n.q, &n.k_cache, &n.v_cache})
     if (requests && pages && common_alignment(*t, 16 / size_of_dtype(dtype)) * size_of_dtype(dtype) != 16)
       return c.fail(FC_E_UNBOUND, "the rows of q and of the caches must be 16-byte aligned").code();
+  // a workgroup counts the elements of a request without keys four at a time, and steps past the last
+  if (heads * (dim / 4) > 0x7fffffff) return c.fail(FC_E_LIMIT, "a request's heads have more than 2^33 elements").code();
   auto op = std::make_unique<PagedAttention>();
   op->dtype = dtype;
   AttentionArgs &a = op->a;

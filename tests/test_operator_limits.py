@@ -61,3 +61,13 @@ def test_heads_that_go_into_the_cache_are_counted_in_full():
     expect("FC_E_LIMIT", of(2, (1 << 30) - 1))
     expect("FC_E_LIMIT", of((1 << 31) - 1, (1 << 31) - 1))
     taken(of(1, (1 << 30) - 1))
+
+
+def test_attention_counts_the_elements_of_a_request_in_full():
+    def of(heads, dim):
+        cache, row = T("bfloat16", 9, 16, 1, dim), T("bfloat16", 1, heads, dim)
+        return attention(q=row, out=row, lse=None, lengths=T("int32", 1), table=T("int32", 1, 8), k_cache=cache, v_cache=cache)
+    for heads_, dim in ((1 << 26, 256), ((1 << 31) - 1, 8), (1 << 30, 8), (1 << 25, 256)):
+        expect("FC_E_LIMIT", of(heads_, dim))
+    for heads_, dim in (((1 << 25) - 1, 256), ((1 << 30) - 1, 8)):
+        taken(of(heads_, dim))
