@@ -368,7 +368,7 @@ typedef struct fc_page_map {
  *   (y[i], y[i + R/2]), interleaved: (y[2i], y[2i + 1]);  (a, b) -> (a c - b s, b c + a s).
  * In 32 bits, rounded once.  Keys go to k_out, or, with values as they are, to row slots[t] of the caches (page slots[t] / P, place
  * slots[t] mod P); slots outside the cache, -1 among them, are skipped; slots of one call are distinct.  A position or an axis outside
- * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides).
+ * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides: FC_E_ARG otherwise).
  * At most 255 axes, 2^31-1 places of the cache and 2^31-1 heads of a token, all of q, k and (with slots) v (FC_E_LIMIT).  Rows are read 16 bytes at a time; where D/2, R/2 (not interleaved), a stride
  * or an alignment does not allow it fewer, and then D is at most 128 times the elements of a read (FC_E_UNSUPPORTED). */
 typedef struct fc_head_norm_rope {
@@ -391,7 +391,7 @@ typedef struct fc_head_norm_rope {
 
 /* Its gradient: dq and dk from the gradients of q_out and k_out, and (f32) those of the weights, summed over tokens and heads in a
  * fixed order.  With g = dy turned back, u = x * rsqrt(mean(x^2) + eps): dweight = sum g u, dx = rsqrt(...) * (w g - u mean(w g u)).
- * dq may be dq_out and dk may be dk_out. */
+ * dq may be dq_out and dk may be dk_out, as above. */
 typedef struct fc_head_norm_rope_grad {
   fc_tensor q, k, q_weight, k_weight, cos_sin, positions, axis_of;   /* as above */
   fc_tensor dq_out;       /* [T, Hq, D] */

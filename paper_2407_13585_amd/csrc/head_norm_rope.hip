@@ -658,6 +658,7 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
   HeadsArgs &a = op->a;
   const int64_t tokens = a.tokens, dim = a.dim, kv = a.heads[1];
   c.array("q_out", n.q_out, op->dtype, {tokens, a.heads[0], dim}, true);
+  if (c.ok() && other_strides(n.q, n.q_out)) c.fail(FC_E_ARG, "q_out is at the address of q with other strides");
   a.q_out = rows_at(n.q_out);
   auto align = [&](const fc_tensor &t) { op->pack = common_alignment(t, op->pack); };
   if (present(n.slots)) {
@@ -685,6 +686,7 @@ int make_head_norm_rope(const fc_head_norm_rope &n, std::unique_ptr<Operator> &o
   } else {
     if (present(n.v) || present(n.k_cache) || present(n.v_cache)) c.fail(FC_E_ARG, "v and the caches go with slots");
     c.array("k_out", n.k_out, op->dtype, {tokens, kv, dim}, true);
+    if (c.ok() && other_strides(n.k, n.k_out)) c.fail(FC_E_ARG, "k_out is at the address of k with other strides");
     a.k_out = rows_at(n.k_out);
     align(n.k_out);
   }
@@ -706,6 +708,8 @@ int make_head_norm_rope_grad(const fc_head_norm_rope_grad &n, std::unique_ptr<Op
   c.array("dk_out", n.dk_out, op->dtype, {tokens, a.heads[1], dim});
   c.array("dq", n.dq, op->dtype, {tokens, a.heads[0], dim}, true);
   c.array("dk", n.dk, op->dtype, {tokens, a.heads[1], dim}, true);
+  if (c.ok() && other_strides(n.dq_out, n.dq)) c.fail(FC_E_ARG, "dq is at the address of dq_out with other strides");
+  if (c.ok() && other_strides(n.dk_out, n.dk)) c.fail(FC_E_ARG, "dk is at the address of dk_out with other strides");
   if (present(n.q_weight) != present(n.dq_weight) || present(n.k_weight) != present(n.dk_weight))
     c.fail(FC_E_ARG, "a weight and its gradient are there together or not at all");
   if (present(n.dq_weight)) c.array("dq_weight", n.dq_weight, FC_F32, {dim}, true);

@@ -77,10 +77,15 @@ class TensorChecks {
 };
 
 inline bool present(const fc_tensor &t) { return t.rank != 0; }
-inline bool same_memory(const fc_tensor &a, const fc_tensor &b) {
-  bool same = a.ptr == b.ptr && a.rank == b.rank;
-  for (int k = 0; same && k < a.rank; ++k) same = a.stride[k] == b.stride[k];
-  return same;
+// Whether `out`, of the shape of `in` and at its address, lies otherwise than `in`, so that rows would be written over before they are
+// read.  An axis along which `in` is one row for all is left to the caller.
+inline bool other_strides(const fc_tensor &in, const fc_tensor &out) {
+  bool differ = false, empty = false;
+  for (int k = 0; k < in.rank; ++k) {
+    differ |= in.shape[k] > 1 && in.stride[k] != 0 && in.stride[k] != out.stride[k];
+    empty |= in.shape[k] == 0;
+  }
+  return in.ptr == out.ptr && differ && !empty;
 }
 inline int size_of_dtype(int32_t dtype) { return dtype == FC_I64 ? 8 : dtype == FC_F16 || dtype == FC_BF16 ? 2 : 4; }
 // the largest power of two, `most` at most, that the base and all strides but the innermost (in elements) are multiples of

@@ -1,5 +1,5 @@
-"""Extents of the operators of a serving cache that their kernels cannot count: refused before anything is enqueued, and what lies just
-below them taken.  No GPU: the arrays are addresses that nothing reads."""
+"""What the operators of a serving cache refuse before anything is enqueued: extents that their kernels cannot count, outputs that lie over
+their inputs otherwise than they do; and what lies just beside it is taken.  No GPU: the arrays are addresses that nothing reads."""
 import pytest
 
 import paper_2407_13585_amd as fc
@@ -71,3 +71,21 @@ def test_attention_counts_the_elements_of_a_request_in_full():
         expect("FC_E_LIMIT", of(heads_, dim))
     for heads_, dim in (((1 << 25) - 1, 256), ((1 << 30) - 1, 8)):
         taken(of(heads_, dim))
+
+
+def test_outputs_in_place_lie_as_their_inputs_do():
+    def lying(heads_, stride, ptr=0x20000000):
+        return T("bfloat16", 7, heads_, 64, stride=stride, ptr=ptr)
+    # the heads' rows of one projection in place, and rows of a single head, whose stride between heads means nothing
+    taken(heads(q=lying(4, (512, 64, 1)), q_out=lying(4, (512, 64, 1))))
+    taken(heads(q=lying(1, (64, 999, 1)), q_out=lying(1, (64, 64, 1)), k=lying(1, (64, 5, 1)), k_out=lying(1, (64, 64, 1))))
+    taken(heads(q_out=lying(4, (64, 448, 1), ptr=0x30000000)))
+    taken(heads(tokens=0, q_out=T("bfloat16", 0, 4, 64, stride=(64, 448, 1))))
+    # the same address, transposed or with gaps
+    for stride in ((64, 448, 1), (512, 64, 1)):
+        expect("FC_E_ARG", heads(q_out=lying(4, stride)))
+        expect("FC_E_ARG", heads(q=lying(4, stride)))
+        expect("FC_E_ARG", into_cache(q_out=lying(4, stride)))
+        expect("FC_E_ARG", heads(True, dq=lying(4, stride)))
+        expect("FC_E_ARG", heads(k_out=lying(2, stride)))
+        expect("FC_E_ARG", heads(True, dk_out=lying(2, stride)))
