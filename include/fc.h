@@ -376,7 +376,7 @@ typedef struct fc_head_norm_rope {
   fc_tensor k;            /* [T, Hk, D] */
   fc_tensor q_weight;     /* [D] of the same type, or absent */
   fc_tensor k_weight;
-  fc_tensor cos_sin;      /* f32 [positions there are, R], R even, R <= D; or absent */
+  fc_tensor cos_sin;      /* f32 [positions there are, R], R even, R <= D; or absent.  Without rows every position is outside it */
   fc_tensor positions;    /* i32 [axes, T]; absent with cos_sin */
   fc_tensor axis_of;      /* i32 [R / 2], or absent */
   fc_tensor q_out;        /* [T, Hq, D], out */

@@ -54,7 +54,7 @@ def angles(cos_sin, positions, axis_of):
     c, s = np.full((tokens, half), np.nan), np.full((tokens, half), np.nan)
     for i in range(half):
         axis = 0 if axis_of is None else int(axis_of[i])
-        if not 0 <= axis < axes:
+        if not (0 <= axis < axes and rows):
             continue
         there = (positions[axis] >= 0) & (positions[axis] < rows)
         at = np.where(there, positions[axis], 0)

@@ -31,13 +31,13 @@ struct HeadsArgs {
   Rows q, k, v, q_out, k_out;       // k_out: the tensor, or place 0 of the cache's pages (head: its stride)
   char *v_cache;
   const void *weight[2];            // of q and of k; NULL: no norm
-  const float *cos_sin;             // NULL: no rotation
+  const float *cos_sin;             // may be NULL where it has no rows
   const int *positions, *axis_of;
   const long long *slots;           // NULL: keys go to the tensor
   long long angle_stride, position_stride;
   long long k_page, k_place, v_page, v_place, v_head;     // strides of the caches
   unsigned tokens, heads[3];        // of q, k, v
-  unsigned dim, half, page, places; // half: R / 2; places: of the cache
+  unsigned dim, half, page, places; // half: R / 2, 0: no rotation; places: of the cache
   unsigned axes, angles;            // rows of positions and of cos_sin
   unsigned lanes_log2, per_wave;    // lanes of a row; heads of a token that a wave takes
   float eps;
@@ -152,7 +152,7 @@ __device__ __forceinline__ unsigned axes_of_lane(const HeadsArgs &a) {
 // one row of the token.
 template <int V, int Pairs>
 __device__ __forceinline__ void load_angles(const HeadsArgs &a, const Place<V, Pairs> &p, unsigned t, float (&c)[V], float (&s)[V]) {
-  if (!a.cos_sin) return;
+  if (!a.half) return;
   constexpr int kAngles = Place<V, Pairs>::kAngles;
   const int at = a.axes ? load_scalar(a.positions + t) : -1;
   const bool there = (unsigned)at < a.angles;
@@ -593,7 +593,7 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
   while (call.pack > 1 && dim / 2 % call.pack) call.pack /= 2;
   for (const fc_tensor *t : {&q, &k, &q_weight, &k_weight})
     if (present(*t)) call.pack = common_alignment(*t, call.pack);
-  a.wide_angles = a.cos_sin && common_alignment(cos_sin, 4) == 4;
+  a.wide_angles = a.half && common_alignment(cos_sin, 4) == 4;
   return FC_OK;
 }
 
