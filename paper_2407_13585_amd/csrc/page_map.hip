@@ -259,7 +259,7 @@ __device__ __forceinline__ void fill(const PageMapArgs &a, const Ring &ring, Sum
   }
   if (a.entries == 0) return;
   // the pages of tokens that have no entry, which nobody above has seen: all pages taken, some a second time
-  if (live > a.tokens)
+  if (all.tokens > a.tokens)
     for (unsigned i = group * Threads + threadIdx.x; i < min(all.taken, ring.available); i += stride) {
       const unsigned r = last_not_above(of.first, a.requests, i);
       a.table[(long long)r * a.table_stride + pages_of(a, of.length[r]) + (i - of.first[r])] = a.pool[Ring::place(a, ring.head, i)];
