@@ -71,16 +71,19 @@ __device__ __forceinline__ Acc mma(Vec<float, 4> a, Vec<float, 4> b, Acc c) {
   return c;
 }
 
-// A weight as two numbers of 16 bits: the upper part cut off, not rounded, so that the rest is not negative, and the rest never 0, so
-// that an infinite value times a weight stays that infinity in both products.  Together 16 bits (bf16) or 22 of the weight.
+// A weight as two numbers of 16 bits: the upper part cut off, not rounded, so that the rest is not negative, and the rest not 0 where the
+// upper part is not, so that an infinite value times a weight stays that infinity in both products.  Together 16 bits (bf16) or 22 of the
+// weight, which leaves a result as exact as its own 16 bits hold it; a third part would make the matrix instructions of the values half as
+// many again.  A weight below the smallest number, 2^-38 of the largest one for f16, is rounded to it or to 0: it must not add
+// up over the keys.  The median is the larger of what is left and the smallest number where the weight is above that, else the weight.
 __device__ __forceinline__ void split(float p, __bf16 &high, __bf16 &low) {
   const float cut = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
   high = (__bf16)cut;
-  low = (__bf16)fmaxf(p - cut, 0x1p-126f);
+  low = (__bf16)__builtin_amdgcn_fmed3f(p - cut, 0x1p-126f, p);
 }
 __device__ __forceinline__ void split(float p, _Float16 &high, _Float16 &low) {
   high = (_Float16)__builtin_amdgcn_cvt_pkrtz(p, 0.0f)[0];
-  low = (_Float16)fmaxf(p - (float)high, 0x1p-24f);
+  low = (_Float16)__builtin_amdgcn_fmed3f(p - (float)high, 0x1p-24f, p);
 }
 
 // 2^shift e^x, x not above 0.  The difference from the maximum is taken before it is put into powers of 2, so that the rounding of large scores

@@ -3,7 +3,7 @@ Tolerances are those of test_gpu_operators.py unless a test says otherwise."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import check_grad, check_heads, gpu, heads_case, host, run
+from test_gpu_operators import check_attention, check_grad, check_heads, gpu, heads_case, host, run, types
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,44 @@ def test_pages_are_entered_for_more_tokens_than_can_be_counted_where_every_count
         assert torch.equal(slots[at], gpu(order)[at // page].long() * page + at % page)
     del slots, positions, request
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,large", [("f32", 1e30), ("f16", 60000.0), ("bf16", 1e35)])
+@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("below", [40.0, 100.0])
+def test_keys_of_no_weight_to_speak_of_add_nothing_however_many_they_are(dtype, large, page, below):
+    # One key has all the weight, each of the others e^-below of it.  Where that is too little for the type's numbers they must add nothing: together they
+    # come to 20000 * e^-40 * 6e4 = 5e-9 for f16, 20000 * e^-100 * 1e35 = 7e-5 for bf16, and to less for f32.
+    import torch
+    keys, dim = 20000, 64
+    if below == 40.0 and dtype != "f16":
+        large = 1e6                                              # 20000 * e^-40 * 1e6 = 8e-8
+    pages = -(-keys // page)
+    k = torch.zeros((pages * page, 1, dim), device="cuda")
+    v = torch.full((pages * page, 1, dim), large, device="cuda")
+    k[:, 0, 0] = -below
+    at = 12345
+    k[at, 0, 0], v[at] = 0.0, 1.0
+    q = torch.zeros((1, 2, dim), device="cuda")
+    q[:, :, 0] = 8.0                                             # times the scale of 1/8: scores of 0 and -below
+    s = {"q": q.to(types()[dtype]), "k_cache": k.view(pages, page, 1, dim).to(types()[dtype]), "v_cache": v.view(pages, page, 1, dim).to(types()[dtype]),
+         "table": torch.arange(pages, dtype=torch.int32, device="cuda")[None], "lengths": gpu(np.array([keys], np.int32))}
+    check_attention(s, dtype)
+
+
+def test_keys_of_no_weight_in_one_wave_s_row_add_nothing_in_16_bits():
+    # 1024 requests of 65536 keys over the same two pages, so that a wave walks 16384 keys after the one that has all the weight.  2^-38 of it for each
+    # of them, the smallest weight that 16 bits hold here, would make 1 + 16384 * 2^-38 * 6e4 = 1.0036 of a result that is 1.
+    import torch
+    import paper_2407_13585_amd as fc
+    requests, keys, page, dim = 1024, 65536, 16, 64
+    half = dict(dtype=torch.float16, device="cuda")
+    k, v = torch.zeros((2, page, 1, dim), **half), torch.full((2, page, 1, dim), 6e4, **half)
+    k[..., 0] = -100.0
+    k[1, 0], v[1, 0] = 0.0, 1.0
+    table = torch.zeros((requests, keys // page), dtype=torch.int32, device="cuda")
+    table[:, 0] = 1
+    q, out, lse = torch.zeros((requests, 1, dim), **half), torch.empty((requests, 1, dim), **half), torch.empty((requests, 1), device="cuda")
+    q[..., 0] = 8.0
+    run([fc.PagedAttention(q=q, k_cache=k, v_cache=v, table=table, lengths=torch.full((requests,), keys, dtype=torch.int32, device="cuda"), out=out, lse=lse)])
+    assert bool((out == 1).all()) and bool((lse == 0).all())
