@@ -1215,6 +1215,12 @@ __global__ __launch_bounds__(kBlock) void foldseg_kernel(const Packed<kHeadAux |
   }
 }
 
+// zeros in Words words, a thread each
+template <int Words> __global__ __launch_bounds__(kBlock) void clear_words_kernel(unsigned *words) {
+  static_assert(Words % kBlock == 0, "whole workgroups");
+  words[blockIdx.x * kBlock + threadIdx.x] = 0u;
+}
+
 // ------------------------------------------------------------------ segmented fold over a gathered table, column blocked
 // y[r] = fold(+, F(values[k], table[index[k]]) for k in segment r) where the table
 // is too large for the L2 of one XCD (4 MiB) but not for four of them.  Random

@@ -100,6 +100,11 @@ template <class Op, class E> hipError_t launch_foldseg(const KArgs &a, const Lau
   if (mean < 256.0) return go(&foldseg_kernel<Op, E, 16, U>, 16);
   return go(&foldseg_kernel<Op, E, kWave, U>, kWave);
 }
+// After a launch whose tiles' words reach into the operators' counters.
+hipError_t launch_clear_counters(const LaunchCtx &c) {
+  std::tuple<unsigned *> vals(reinterpret_cast<unsigned *>(reinterpret_cast<char *>(c.ctl) + kCountersOffset));
+  return launch_impl(&clear_words_kernel<kCounters>, dim3(kCounters / kBlock), dim3(kBlock), c, vals, std::index_sequence_for<unsigned *>());
+}
 // ---- column-blocked segmented fold: for tables of more than one and at most four L2s ----
 constexpr size_t kL2Bytes = 4u << 20;                 // L2 of one XCD
 template <int KT> size_t blocked_table_bytes(const KArgs &a) {
@@ -123,8 +128,9 @@ hipError_t launch_foldseg_blocked(const KArgs &a, const LaunchCtx &c) {
   grid = std::max(8u, std::min(grid, units * kQuarters / 8 * 8));
   const size_t elems = blocked_table_bytes<KT>(a) / 4;
   const int range_len = (int)(((elems + kQuarters - 1) / kQuarters + 31) / 32 * 32);    // whole 128-byte lines
-  return launch_k(&foldseg_blocked_kernel<Op, F, KV, KI, KT>, grid, c, a, c.ctl, c.partials, c.status,
-                  static_cast<unsigned long long *>(c.workspace), range_len);
+  const hipError_t e = launch_k(&foldseg_blocked_kernel<Op, F, KV, KI, KT>, grid, c, a, c.ctl, c.partials, c.status,
+                                static_cast<unsigned long long *>(c.workspace), range_len);
+  return e == hipSuccess && (size_t)units * kQuarters > kFreeTiles ? launch_clear_counters(c) : e;
 }
 
 // ---- fold over a gathered table of one to sixty-four L2s: indices sorted by table range first ----
@@ -326,6 +332,7 @@ hipError_t launch_foldseg_sorted(const KArgs &a, const LaunchCtx &c) {
                   static_cast<const T *>(head), static_cast<const T *>(tail), p.tiles);
 }
 
+static_assert(2 * ((1ull << 31) / scan_tile(kScanFAcc < kScanAcc ? kScanFAcc : kScanAcc)) <= kFreeTiles, "the words of no scan reach into the counters");
 template <class EX, class EV, int Mode, bool Reverse, int Acc> hipError_t launch_scan_of(const KArgs &a, const LaunchCtx &c) {
   const unsigned tiles = scan_tiles((unsigned)a.n, (unsigned)scan_tile(Acc));
   if (scan_status_words(tiles) > c.max_tiles) return hipErrorInvalidValue;

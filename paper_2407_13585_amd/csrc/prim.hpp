@@ -157,10 +157,12 @@ struct Control {
 constexpr int kMaxPartials = 8192;                 // workgroups of a fold launch
 constexpr size_t kPartialsOffset = sizeof(Control);
 constexpr size_t kStatusOffset = kPartialsOffset + kMaxPartials * sizeof(unsigned long long);
-// counters of workgroups that are done with their part of something (operators): 0 between launches, the last to count resets them
+constexpr size_t kMaxTiles = (FC_SCRATCH_CONTROL_BYTES - kStatusOffset) / sizeof(unsigned long long);
+// Counters of workgroups that are done with their part of something (operators): 0 between launches, the last to count resets them.  They lie
+// over the last tiles' words: a launch that uses more than kFreeTiles of these is followed by one that clears them.
 constexpr int kCounters = 4096;
 constexpr size_t kCountersOffset = FC_SCRATCH_CONTROL_BYTES - kCounters * sizeof(unsigned);
-constexpr size_t kMaxTiles = (kCountersOffset - kStatusOffset) / sizeof(unsigned long long);
+constexpr size_t kFreeTiles = (kCountersOffset - kStatusOffset) / sizeof(unsigned long long);
 constexpr unsigned kSpinLimit = 1u << 22;          // polls before a wait gives up: never hang the device
 
 // `epoch` read at the very start of a kernel, with an ordinary load.  The word changes only once

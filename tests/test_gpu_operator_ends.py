@@ -87,3 +87,37 @@ def test_keys_of_no_weight_in_one_wave_s_row_add_nothing_in_16_bits():
     q[..., 0] = 8.0
     run([fc.PagedAttention(q=q, k_cache=k, v_cache=v, table=table, lengths=torch.full((requests,), keys, dtype=torch.int32, device="cuda"), out=out, lse=lse)])
     assert bool((out == 1).all()) and bool((lse == 0).all())
+
+
+def test_operators_share_the_scratch_of_a_segmented_fold_of_as_many_rows_as_its_flags_allow():
+    # 66.5 million rows, an element in every sixteenth: the column-blocked fold's flags reach into the operators' counters, which are left cleared
+    import torch
+    import paper_2407_13585_amd as fc
+    from paper_2407_13585_amd import binding as B
+    from test_gpu_operators import attention_case, attention_want, near
+    from test_operator_limits import spmv_of_many_rows
+    rows, cols = 66500000, 1500000
+    elements = -(-rows // 16)
+    g, part = spmv_of_many_rows(rows, elements, cols)
+    assert "column-blocked" in fc.fc_cluster_kernel(g, part, 0)
+    gen = torch.Generator("cuda").manual_seed(1)
+    x, vals = (torch.rand(n, generator=gen, device="cuda") + 0.5 for n in (cols, elements))
+    col = torch.randint(0, cols, (elements,), generator=gen, device="cuda", dtype=torch.int32)
+    off = ((torch.arange(rows + 1, device="cuda") + 15) // 16).int()
+    y, want = torch.empty(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    want[::16] = vals * x[col.long()]
+    scratch = torch.zeros(fc.fc_scratch_bytes(g, part), dtype=torch.uint8, device="cuda")
+    fold = B.BoundRun(g, part, {"x": x, "col": col, "vals": vals, "off": off, "y": y}, scratch)
+    s = attention_case([5000, 900], 4, 2, 64, 16, "f32", seed=1)
+    out, lse = torch.empty((2, 4, 64), device="cuda"), torch.empty((2, 4), device="cuda")
+    attend = fc.BoundOperators([fc.PagedAttention(out=out, lse=lse, **s)], scratch)
+    ref, ref_lse, _, _ = attention_want(s, 0.125, 0)
+    for _ in range(3):
+        for t in (y, out, lse):
+            t.fill_(7.0)
+        fold(torch.cuda.current_stream().cuda_stream)
+        attend(torch.cuda.current_stream().cuda_stream)
+        fc.fc_check(scratch, torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(y, want)
+        near(host(out), ref, 1e-5)
+        near(host(lse), ref_lse, 1e-5)

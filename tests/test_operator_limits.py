@@ -3,7 +3,9 @@ their inputs otherwise than they do; and what lies just beside it is taken.  No 
 import pytest
 
 import paper_2407_13585_amd as fc
+from paper_2407_13585_amd import binding as B
 from test_operators import SCRATCH, T, attention, heads, into_cache
+from workloads import Graph
 
 
 def expect(code, *ops):
@@ -89,3 +91,25 @@ def test_outputs_in_place_lie_as_their_inputs_do():
         expect("FC_E_ARG", heads(True, dq=lying(4, stride)))
         expect("FC_E_ARG", heads(k_out=lying(2, stride)))
         expect("FC_E_ARG", heads(True, dk_out=lying(2, stride)))
+
+
+def spmv_of_many_rows(rows, elements, cols=1500000):
+    g = Graph()
+    g.add("x", "input", "f32", (cols,))
+    g.add("col", "input", "i32", (elements,))
+    g.add("vals", "input", "f32", (elements,))
+    g.add("off", "input", "i32", (rows + 1,))
+    g.add("g", "gather", "f32", (elements,), args=("col", "x"))
+    g.add("p", "map", "f32", (elements,), fn="mul2", args=("vals", "g"))
+    g.add("y", "foldseg", "f32", (rows,), fn="add", args=("p", "off"), output=True)
+    return g, fc.fc_plan(g, "bytes")
+
+
+@pytest.mark.parametrize("elements", [4000000, (1 << 28) + 1, (1 << 29) - 1])          # what the fold that sorts its elements leaves to this one
+def test_a_segmented_fold_takes_the_rows_it_took_without_the_operators_counters(elements):
+    # four flags of 8 bytes for every 256 rows, in what the control block leaves behind its first 65792 bytes
+    most = (B.FC_SCRATCH_CONTROL_BYTES - 256 - 65536) // 32 * 256
+    for rows, blocked in ((66450000, True), (66500000, True), (most, True), (most + 1, False)):
+        g, part = spmv_of_many_rows(rows, elements)
+        assert ("column-blocked" in fc.fc_cluster_kernel(g, part, 0)) == blocked, rows
+        assert (fc.fc_scratch_bytes(g, part) >= B.FC_SCRATCH_CONTROL_BYTES + 32 * rows) == blocked, rows
