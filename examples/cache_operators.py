@@ -12,6 +12,7 @@ import sys
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2407_13585_amd as fc  # noqa: E402
@@ -98,7 +99,8 @@ class Server:
 
 
 class HeadNormRopeFunction(torch.autograd.Function):
-    """q, k [T, heads, D], norm weights [D], angles as HeadNormRope takes them -> q and k normed and turned."""
+    """q, k [T, heads, D], norm weights [D], angles as HeadNormRope takes them -> q and k normed and turned.  Differentiable once: backward
+    is a kernel itself, and a gradient of it is refused."""
 
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, cos_sin, positions):
@@ -109,6 +111,7 @@ class HeadNormRopeFunction(torch.autograd.Function):
         return q_out, k_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, cos_sin, positions = ctx.saved_tensors
         dq, dk = torch.empty_like(q), torch.empty_like(k)

@@ -134,3 +134,14 @@ def test_the_function_has_the_gradient_of_the_formula(example):
     torch.autograd.backward([formula(there[0], there[2]), formula(there[1], there[3])], [d.double() for d in dy])
     for x, y, n in zip(here, there, (1, 1, 33 * 5, 33 * 2)):
         assert float((x.grad.double() - y.grad).abs().max()) <= 6e-5 * n
+
+
+def test_a_gradient_of_the_function_s_gradient_is_refused(example):
+    # backward is not made of differentiable steps: without the refusal the sum's gradient would come out as that of its second term alone
+    import torch
+    q, k = (torch.randn(5, h, 16, device="cuda", requires_grad=True) for h in (2, 1))
+    weights = [torch.ones(16, device="cuda", requires_grad=True) for _ in range(2)]
+    out_q, _ = example.HeadNormRopeFunction.apply(q, k, *weights, example.angle_table(9, 16, "cuda"), torch.zeros((1, 5), dtype=torch.int32, device="cuda"))
+    slope, = torch.autograd.grad(out_q.square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (slope.square().sum() + q.square().sum()).backward()
