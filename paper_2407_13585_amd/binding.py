@@ -7,6 +7,7 @@ Device memory and streams come from the caller (torch tensors or raw pointers).
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -519,13 +520,17 @@ def _tensor(x) -> fc_tensor:
 
 
 class CacheOperator:
-    """One operator on the caller's tensors, which live as long as this object.  Every check is the library's."""
+    """One operator on the caller's tensors, which live as long as this object.  Every check but that numbers fit the ABI's is the
+    library's."""
 
     kind = -1
     struct = None
 
     def _describe(self, tensors: Dict[str, object], **scalars) -> None:
         self.tensors = tensors
+        for name, kind in self.struct._fields_:
+            if kind is C.c_int32 and not -1 << 31 <= operator.index(scalars[name]) < 1 << 31:     # ctypes would cut it to its last 32 bits
+                raise ValueError(f"{name} = {scalars[name]} does not fit 32 bits")
         self.c = self.struct(**scalars)
         for name, x in tensors.items():
             setattr(self.c, name, _tensor(x))

@@ -4,7 +4,7 @@ import pytest
 
 import paper_2407_13585_amd as fc
 from paper_2407_13585_amd import binding as B
-from test_operators import SCRATCH, T, attention, heads, into_cache
+from test_operators import SCRATCH, T, attention, heads, into_cache, page_map
 from workloads import Graph
 
 
@@ -91,6 +91,16 @@ def test_outputs_in_place_lie_as_their_inputs_do():
         expect("FC_E_ARG", heads(True, dq=lying(4, stride)))
         expect("FC_E_ARG", heads(k_out=lying(2, stride)))
         expect("FC_E_ARG", heads(True, dk_out=lying(2, stride)))
+
+
+def test_numbers_that_the_abi_would_cut_short_are_refused():
+    for make in (lambda n: attention(window=n), lambda n: page_map(page_size=n)):
+        for n in (1 << 31, (1 << 32) + 16, 1 << 64, -(1 << 31) - 1):
+            with pytest.raises(ValueError, match="32 bits"):
+                make(n)
+        taken(make((1 << 31) - 1))
+    with pytest.raises(TypeError):
+        attention(window=16.0)
 
 
 def spmv_of_many_rows(rows, elements, cols=1500000):
