@@ -562,6 +562,7 @@ int check_heads(TensorChecks &c, const fc_tensor &q, const fc_tensor &k, const f
     c.fail(FC_E_ARG, "positions and axis_of go with cos_sin");
   }
   if (c.ok() && !(eps >= 0 && std::isfinite((float)eps))) c.fail(FC_E_ARG, "eps must be finite, in 32 bits too, and not negative");
+  if (c.ok() && eps > 0 && (float)eps == 0) c.fail(FC_E_ARG, "eps is 0 in 32 bits");      // rows of zeros would be NaN
   if (c.ok() && (dim < 2 || dim % 2 || dim > (int64_t)kMostDim)) c.fail(FC_E_UNSUPPORTED, "heads have an even number of elements, at most 512");
   // a token's heads, those of values among them, are numbered in one row, which a wave walks in steps of up to 64 that must not pass 32 bits
   if (c.ok() && (q.shape[1] + (values ? 2 : 1) * k.shape[1] > 0x7fffffff || tokens * (q.shape[1] + k.shape[1]) > (int64_t)1 << 40)) c.fail(FC_E_LIMIT, "too many heads");

@@ -103,6 +103,15 @@ def test_numbers_that_the_abi_would_cut_short_are_refused():
         attention(window=16.0)
 
 
+@pytest.mark.parametrize("grad", [False, True])
+def test_an_eps_that_32_bits_take_for_zero_is_refused(grad):
+    # 2^-149 is the smallest number of 32 bits, half of it is rounded to 0: a row of zeros would be NaN, not zeros
+    for eps in (2.0 ** -150, 1e-46, 1e-300):
+        expect("FC_E_ARG", heads(grad, eps=eps))
+    for eps in (0.0, 2.0 ** -149, 1e-38):
+        taken(heads(grad, eps=eps))
+
+
 def spmv_of_many_rows(rows, elements, cols=1500000):
     g = Graph()
     g.add("x", "input", "f32", (cols,))
