@@ -3,7 +3,7 @@ Tolerances are those of test_gpu_operators.py unless a test says otherwise."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import check_attention, check_grad, check_heads, gpu, heads_case, host, run, types
+from test_gpu_operators import LENGTHS, TINY, U, attention_case, attention_want, check_attention, check_grad, check_heads, gpu, heads_case, host, near, run, types
 
 pytestmark = pytest.mark.gpu
 
@@ -89,12 +89,23 @@ def test_keys_of_no_weight_in_one_wave_s_row_add_nothing_in_16_bits():
     assert bool((out == 1).all()) and bool((lse == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("dim,page,window", [(8, 16, 0), (64, 16, 0), (64, 7, 90), (80, 24, 0), (96, 24, 200), (128, 32, 0), (128, 3, 0), (192, 16, 0), (256, 5, 0)])
+def test_attention_holds_weights_in_more_than_16_bits(dtype, dim, page, window):
+    # check_attention allows every type what bf16 needs, 2^-16 of a weight.  f32 has its weights in full and f16 in 22 bits: what is left is the error of
+    # the scores and 2^-20 for powers and sums, twice, and the result's own rounding.
+    s = attention_case(LENGTHS + [3000], 6, 3, dim, page, dtype, seed=dim + page)
+    out, _ = check_attention(s, dtype, window=window)
+    ref, _, reach, spread = attention_want(s, dim ** -0.5, window)
+    weight = (dim + 8) * 2.0 ** -24 * reach[..., None] + 2.0 ** -20 + (2.0 ** -22 if dtype == "f16" else 0.0)
+    near(out, ref, 2 * weight * spread + U[dtype] * np.abs(ref) + TINY[dtype], "out")
+
+
 def test_operators_share_the_scratch_of_a_segmented_fold_of_as_many_rows_as_its_flags_allow():
     # 66.5 million rows, an element in every sixteenth: the column-blocked fold's flags reach into the operators' counters, which are left cleared
     import torch
     import paper_2407_13585_amd as fc
     from paper_2407_13585_amd import binding as B
-    from test_gpu_operators import attention_case, attention_want, near
     from test_operator_limits import spmv_of_many_rows
     rows, cols = 66500000, 1500000
     elements = -(-rows // 16)
