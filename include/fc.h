@@ -369,8 +369,9 @@ typedef struct fc_page_map {
  * In 32 bits, rounded once.  Keys go to k_out, or, with values as they are, to row slots[t] of the caches (page slots[t] / P, place
  * slots[t] mod P); slots outside the cache, -1 among them, are skipped; slots of one call are distinct.  A position or an axis outside
  * its table gives NaN in the rotated elements that need it.  q_out may be q and k_out may be k (same memory, same strides: FC_E_ARG otherwise).
- * At most 255 axes, 2^31-1 places of the cache and 2^31-1 heads of a token, all of q, k and (with slots) v (FC_E_LIMIT).  Rows are read 16 bytes at a time; where D/2, R/2 (not interleaved), a stride
- * or an alignment does not allow it fewer, and then D is at most 128 times the elements of a read (FC_E_UNSUPPORTED). */
+ * At most 255 axes, 2^31-1 places of the cache and 2^31-1 heads of a token, all of q, k and (with slots) v (FC_E_LIMIT).  With N elements the
+ * largest power of two, of 16 bytes at most, that D/2, R/2 (not interleaved), the strides and the alignment of the rows are multiples
+ * of, D is at most 128 N (FC_E_UNSUPPORTED); rows are read N elements at a time, or more where R/2 alone makes N one or two. */
 typedef struct fc_head_norm_rope {
   fc_tensor q;            /* [T, Hq, D]: f32, f16 or bf16; D even, at most 512 */
   fc_tensor k;            /* [T, Hk, D] */
@@ -408,6 +409,8 @@ typedef struct fc_head_norm_rope_grad {
  * [max(0, len - window), len), len = lengths[b] (window 0: all), at place j mod P of page table[b][j / P]; keys on pages that are
  * outside the cache or the table are not there.  Query head h reads key head h / (Hq / Hk).
  *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
+ * In 32 bits, rounded once, but for the weights exp(s_j - max) of 16-bit values: two numbers of 16 bits hold them, together 16 bits of a
+ * weight (bf16) or 22, and those below 2^-39 of the largest count as none (f16).
  * A request without keys gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key head, of as many keys as its
  * table could hold, 2^31-1 at most) are counted in 31 bits, the elements of a request's heads, four at a time, too (FC_E_LIMIT).  What lies
  * in the pages past a request's length is not looked at, whatever it holds. */

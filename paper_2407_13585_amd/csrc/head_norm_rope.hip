@@ -7,9 +7,12 @@
 // squares, and the row is read once and written once.  A wave takes one token after the other with some of its heads, so that
 // the token's cosines and sines and the weights are read once and stay in registers.  Memory bounds it where it is large, the launch and a chain
 // of reads (position, angles, result) where it is small:
-//   16384 tokens of 40 heads of 128 (bf16, 338 MB) 61.2 us, 5.5 TB/s; 5003 tokens of 16 heads of 80 with three axes (f16, 27 MB) 10.9 us;
-//   64 tokens into the cache 5.9 us; the gradient of the first (505 MB) with the sum of the weights' gradients 96.7 us, 5.2 TB/s, of 1237
-//   tokens of 12 heads of 64 (f32, 11.6 MB) 10.1 us, a third of them the second launch.
+//   16384 tokens of 40 heads of 128 (bf16, 338 MB) 60.0 to 60.7 us, 5.6 TB/s; 8192 tokens of 28 (f32, 237 MB) 44.8 us, 5.3 TB/s; 5003 tokens of 16 heads
+//   of 80 with three axes (f16, 27 MB) 10.0 to 10.3 us; 64 tokens into the cache 4.7 to 6.0 us; the gradient of the first (505 MB) with the sum
+//   of the weights' gradients 92 to 96 us, 5.3 to 5.5 TB/s, of 1237 tokens of 12 heads of 64 (f32, 11.6 MB) 10.4 us, a third of them the second launch.
+// Rows that do not fill their lanes are bound by instructions: 12844 tokens of 28 heads (bf16) of 72, 80, 96 and 112 elements, turned as a whole or (112)
+// a quarter, 28.9, 30.5, 35.1 and 41.9 us (3.6 to 4.0 TB/s), a quarter of 72 or 80 turned 37.7; their gradients 45.3, 54.1, 57.0 and 69.7,
+// a quarter turned 57.3 and 65.7 (2.6 to 3.7 TB/s).
 #include "operators.hpp"
 
 #include <algorithm>
@@ -108,7 +111,7 @@ __device__ __forceinline__ Packs<T, V> load_packs(const T *row, const Place<V, P
 template <class T, int V, int Pairs> __device__ __forceinline__ void unpack(const Packs<T, V> &w, const Place<V, Pairs> &, float (&x)[2][V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if constexpr (Pairs == kNeighbours) {    // also behind the rotated part: the two packs follow each other there
+    if constexpr (Pairs == kNeighbours) {    // a pair lies in a pack, or is the two packs where these are an element each, side by side
       const int e = 2 * i, o = 2 * i + 1;
       x[0][i] = e < V ? (float)w.a[e % V] : (float)w.b[e % V];
       x[1][i] = o < V ? (float)w.a[o % V] : (float)w.b[o % V];
@@ -300,7 +303,7 @@ struct Turn {
 };
 
 // 1 / sqrt(x) by the instruction (1 ulp; 5003 tokens of 16 heads 10.9 us, 11.3 by root and quotient), which takes what is below the normal numbers
-// for 0
+// for 0.  The mean before it is a product with 1 / D as 32 bits hold it, half a unit more in its last place than a quotient, of which the root leaves half.
 __device__ __forceinline__ float inverse_root(float x) {
   if (__any(x < 0x1p-126f)) return 1.0f / sqrtf(x);
   return __builtin_amdgcn_rsqf(x);
@@ -369,7 +372,8 @@ struct GradRows {
   Rows dy[2], dx[2];                        // of q and of k
 };
 
-// dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].
+// dx, and this workgroup's sums of the weights' gradients: partial[group][q, k][D].  Registers are for three workgroups a compute unit: 16-bit rows with
+// neighbours paired and one axis leave 6 to 10 vector registers of them in memory (28 to 44 bytes a lane), and most forms with several axes 20 bytes.
 template <class T, int V, int Pairs, bool Stream, bool Axes>
 __global__ __launch_bounds__(kThreads, 3) void heads_grad_kernel(HeadsArgs a, GradRows rows_of, float *partial) {
   constexpr bool kCross = Pairs == kCrossed;

@@ -94,11 +94,6 @@ int common_alignment(const fc_tensor &t, int most);
 inline unsigned ceil_div(unsigned long long a, unsigned long long b) { return (unsigned)((a + b - 1) / b); }
 
 // ------------------------------------------------------------------ device
-template <int Dtype> struct ElementOf;
-template <> struct ElementOf<FC_F32> { using T = float; };
-template <> struct ElementOf<FC_F16> { using T = _Float16; };
-template <> struct ElementOf<FC_BF16> { using T = __bf16; };
-
 template <class T, int N> using Vec = T __attribute__((ext_vector_type(N)));      // aligned to its size
 
 // Stream: past the caches, for what is used once (16 bytes)

@@ -6,8 +6,10 @@
 // reads of one token.  Up to 4096 requests every workgroup sums all of them for itself and keeps the sums in LDS, which makes a
 // step one launch (1024 threads a workgroup; 256 up to 1024 requests, whose barriers and scans are shorter); above, two kernels
 // leave the sums in scratch for the third.  What there is of each request is written by a workgroup of its own.
-//   64 requests, a token each: 5.8 us (the launch is about 3.5 of it); 1000 requests, 60013 tokens (1.2 MB): 7.0 us (7.6 with 1024 threads a workgroup);
-//   4096 requests, 2^20 tokens (17 MB): 11.5 us, 1.5 TB/s (17.8 with a token a thread): the sums, a search in LDS, a page and a store one behind another.
+//   64 requests, a token each: 5.5 to 6.1 us (the launch is about 3.5 of it); 1000 requests, 60013 tokens (1.2 MB): 6.9 us (7.6 with 1024 threads a workgroup);
+//   4096 requests, 2^20 tokens (17 MB): 11.5 us, 1.5 TB/s (17.8 with a token a thread): the sums, a search in LDS, a page and a store one behind another,
+//   588 vector instructions a wave, many of them divisions by the page size; a token each 8.3 us, of 4097 requests in three launches 21.5 us;
+//   65536 requests, 2^20 tokens 29.5 us.
 #include "operators.hpp"
 
 namespace fc {

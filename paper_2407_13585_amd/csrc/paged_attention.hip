@@ -19,9 +19,11 @@
 // they are many, a wave takes one at a time instead, and nothing is exchanged at all.
 //
 // Reading the cache once bounds it where that is long, the launch and a chain of reads (lengths, page, keys, pieces) where it is not:
-//   one request of 131072 keys, 8 key heads of 128, 64 heads (bf16, 537 MB) 88 us, 6.1 TB/s; 64 requests of 1 to 8192 keys, 8 key heads of 128 (bf16)
-//   169 us, 6.3 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB) 31.5 us, 3.5 TB/s, where the six
-//   units of a workgroup are too few to hide its start and end; 4 requests of up to 300 keys, 2 key heads of 64 (f16) 7.0 us.
+//   one request of 131072 keys, 8 key heads of 128, 64 heads (bf16, 537 MB) 85 to 88 us, 6.1 to 6.3 TB/s; 64 requests of 1 to 8192 keys, 254057 together,
+//   8 key heads of 128 (bf16, 1041 MB) 179 us, 5.8 TB/s, over pages of 24, 8 or 1 205 us, 5.1 TB/s; 16 requests of 16384 keys, 8 key heads
+//   of 256 (bf16, 2147 MB) 313 us, 6.9 TB/s, of 192 253 us, 6.4 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB)
+//   28 to 30 us, 3.7 to 4.0 TB/s, where the six units of a workgroup are too few to hide its start and end; 4 requests of up to 300 keys,
+//   2 key heads of 64 (f16) 7.1 us.
 #include "operators.hpp"
 
 #include <algorithm>
@@ -255,7 +257,8 @@ template <class T, int Dim, bool Even> struct Wave {
   __device__ __forceinline__ bool inside(unsigned j) const { return j - s.begin < s.end - s.begin; }       // s.end > s.begin
 
   // Whether there is anything of a head in chunk c.  The last quarter of them is left out where it is not, but only where a chunk is four slow matrix
-  // instructions and the pages are of any size (96 elements of 32 bits, pages of 24: 39.5 us, 41.6 without; 16 bits or even pages lose 2 to 7 %).
+  // instructions and the pages are of any size: 37 requests of up to 3001 keys, pages of 24 and 7, heads of 40, 48, 72, 96, 160 and 192 elements of
+  // 32 bits take 2 to 7 % less so (96 elements 40.6 us, 43.2 without), of 112 1 %, of 128 and 256 the same; 16 bits or even pages lose 2 to 7 %.
   __device__ __forceinline__ bool in_use(int c) const { return sizeof(T) == 2 || Even || c < kChunks * 3 / 4 || (unsigned)(c * 4 * kWide) < a.dim; }
 
   __device__ __forceinline__ Where locate(unsigned j0) const {
@@ -479,6 +482,11 @@ template <class T, int Dim, bool Even> struct Wave {
   }
 };
 
+// log sum of a row; the logarithm is the instruction's (1 ulp) of a sum that is never below 2^kShift
+template <class T> __device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? -__builtin_inff() : m + (__log2f(l) - (float)Kind<T>::kShift) * kLn2;
+}
+
 // A row that one wave has done: its lanes write what they hold.
 template <class W, class T> __device__ __forceinline__ void write_wave(const AttentionArgs &a, const W &w, unsigned b, unsigned head0, unsigned count, float l, T *) {
   if (w.r >= count) return;
@@ -499,7 +507,7 @@ template <class W, class T> __device__ __forceinline__ void write_wave(const Att
 #pragma unroll
         for (int e = 0; e < W::kPart; ++e) to[d + e] = x[e];
     }
-  if (a.lse && w.g == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : w.m + (__log2f(l) - (float)Kind<T>::kShift) * kLn2;
+  if (a.lse && w.g == 0) a.lse[b * a.lse_request + head] = log_sum<T>(w.m, l);
 }
 
 template <class T> __device__ __forceinline__ void write_result(const AttentionArgs &a, unsigned b, unsigned head, unsigned d, Vec<float, 4> sum, float m, float l) {
@@ -509,7 +517,7 @@ template <class T> __device__ __forceinline__ void write_result(const AttentionA
   T *to = reinterpret_cast<T *>(a.out) + b * a.out_request + head * a.out_head + d;
 #pragma unroll
   for (int i = 0; i < 4; ++i) to[i] = x[i];
-  if (a.lse && d == 0) a.lse[b * a.lse_request + head] = l == 0.0f ? -__builtin_inff() : m + (__log2f(l) - (float)Kind<T>::kShift) * kLn2;
+  if (a.lse && d == 0) a.lse[b * a.lse_request + head] = log_sum<T>(m, l);
 }
 
 // A piece: the weighted sums of the heads, then (m, l) of each.  It is written and read around the caches that compute units do not
@@ -603,6 +611,8 @@ template <class Slot, class Use> __device__ __forceinline__ void join(const Atte
   }
 }
 
+// A kernel keeps 80 to 239 of its scalars (arguments, strides, descriptors) in lanes of vector registers, the more the larger its heads, and no vector
+// register in memory; heads of more than 128 elements take more than 256 registers, so that a SIMD has one wave.
 template <class T, int Dim, bool Even>
 __global__ __launch_bounds__(kThreads, Dim == 256 ? 1 : Dim == 128 ? (Even && sizeof(T) == 2 ? 3 : 2) : Even ? 4 : 3) void attention_kernel(AttentionArgs a) {
   __shared__ float sums[kWaves][kColumns][Dim + 4];          // + 4: the heads' rows start at different banks
