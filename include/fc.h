@@ -411,8 +411,8 @@ typedef struct fc_head_norm_rope_grad {
  *   s_j = scale q.k_j, out = sum_j exp(s_j) v_j / sum_j exp(s_j), lse = log sum_j exp(s_j)
  * In 32 bits, rounded once, but for the weights exp(s_j - max) of 16-bit values: two numbers of 16 bits hold them, together 16 bits of a
  * weight (bf16) or 22, and those below 2^-39 of the largest count as none (f16).
- * A request without keys gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key head, of as many keys as its
- * table could hold, 2^31-1 at most) are counted in 31 bits, the elements of a request's heads, four at a time, too (FC_E_LIMIT).  What lies
+ * A request without keys, or with no score above -inf, gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key
+ * head, of as many keys as its table could hold, 2^31-1 at most) are counted in 31 bits, the elements of a request's heads, four at a time, too (FC_E_LIMIT).  What lies
  * in the pages past a request's length is not looked at, whatever it holds. */
 typedef struct fc_paged_attention {
   fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */

@@ -3,7 +3,7 @@ Tolerances are those of test_gpu_operators.py unless a test says otherwise."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import LENGTHS, TINY, U, attention_case, attention_want, check_attention, check_grad, check_heads, gpu, heads_case, host, near, run, types
+from test_gpu_operators import LENGTHS, TINY, U, attention_case, attention_raw, attention_want, check_attention, check_grad, check_heads, gpu, heads_case, host, near, run, types
 
 pytestmark = pytest.mark.gpu
 
@@ -99,6 +99,25 @@ def test_attention_holds_weights_in_more_than_16_bits(dtype, dim, page, window):
     ref, _, reach, spread = attention_want(s, dim ** -0.5, window)
     weight = (dim + 8) * 2.0 ** -24 * reach[..., None] + 2.0 ** -20 + (2.0 ** -22 if dtype == "f16" else 0.0)
     near(out, ref, 2 * weight * spread + U[dtype] * np.abs(ref) + TINY[dtype], "out")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("page", [16, 5])
+def test_scores_that_are_all_minus_infinity_leave_what_no_keys_leave(dtype, page):
+    # one element of every key of requests 0 and 1, whose key head is 0, is infinite and that of its queries negative; the other heads keep their keys
+    s = attention_case([1, 700, 700], 4, 2, 64, page, dtype, seed=page)
+    q = s["q"]
+    q[:2, :2, 3] = -abs(q[:2, :2, 3]) - 1
+    table = host(s["table"])
+    for b, n in ((0, 1), (1, 700)):
+        for j in range(n):
+            s["k_cache"][int(table[b, j // page]), j % page, 0, 3] = float("inf")
+    before = attention_want({**s, "k_cache": s["k_cache"].nan_to_num(posinf=0.0), "v_cache": s["v_cache"].nan_to_num()}, 0.125, 0)
+    out, lse = (host(t) for t in attention_raw(s))
+    assert (out[:2, :2] == 0).all() and (lse[:2, :2] == -np.inf).all()
+    for b, h in ((0, 2), (0, 3), (1, 2), (1, 3), (2, 0), (2, 1), (2, 2), (2, 3)):
+        near(out[b, h], before[0][b, h], 2.0 ** -7 if dtype != "f32" else 1e-4)
+        near(lse[b, h:h + 1], before[1][b, h:h + 1], 1e-4)
 
 
 def test_operators_share_the_scratch_of_a_segmented_fold_of_as_many_rows_as_its_flags_allow():
