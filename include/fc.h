@@ -294,7 +294,9 @@ int fc_unbind(fc_bound *b);
 /* The pattern of this library -- index arrays decide what a reduction reads and a scatter writes, and nothing in between
  * reaches memory -- at the place where language models meet it: a cache of keys and values in pages.  FC_PAGE_MAP scans the
  * requests' lengths into block tables and slot maps, FC_HEAD_NORM_ROPE writes keys and values through the slot map,
- * FC_PAGED_ATTENTION folds over the cache gathered through the block table.  The language above cannot say them (rank 2,
+ * FC_PAGED_ATTENTION folds over the cache gathered through the block table.  Three more leave most of a long cache unread:
+ * FC_PAGE_BOUNDS folds the keys of a page into their least and largest, FC_PAGE_SELECT picks by these the pages of a request that each key
+ * head reads, and FC_PREFIX_ATTENTION reads what many requests begin with once for all of them.  The language above cannot say them (rank 2,
  * 32-bit elements, a closed vocabulary), so each is an operator of its own.
  *
  * An operator is a kind and a struct of its arrays.  Lists of operators run in order on a stream under the rules of programs:
@@ -322,7 +324,10 @@ typedef enum fc_operator_kind {
   FC_PAGE_MAP            = 0,  /* args: fc_page_map            */
   FC_HEAD_NORM_ROPE      = 1,  /* args: fc_head_norm_rope      */
   FC_HEAD_NORM_ROPE_GRAD = 2,  /* args: fc_head_norm_rope_grad */
-  FC_PAGED_ATTENTION     = 3   /* args: fc_paged_attention     */
+  FC_PAGED_ATTENTION     = 3,  /* args: fc_paged_attention     */
+  FC_PAGE_BOUNDS         = 4,  /* args: fc_page_bounds         */
+  FC_PAGE_SELECT         = 5,  /* args: fc_page_select         */
+  FC_PREFIX_ATTENTION    = 6   /* args: fc_prefix_attention    */
 } fc_operator_kind;
 
 typedef struct fc_operator {
@@ -413,18 +418,77 @@ typedef struct fc_head_norm_rope_grad {
  * weight (bf16) or 22, and those below 2^-39 of the largest count as none (f16).
  * A request without keys, or with no score above -inf, gets zeros and -inf.  Pieces of a call's work (at most 128 keys of a request's key
  * head, of as many keys as its table could hold, 2^31-1 at most) are counted in 31 bits, the elements of a request's heads, four at a time, too (FC_E_LIMIT).  What lies
- * in the pages past a request's length is not looked at, whatever it holds. */
+ * in the pages past a request's length is not looked at, whatever it holds.
+ * With a table of rank 3 every key head has keys of its own: h sees the lengths[b][h] keys that lie, one page after the other, on the pages
+ * table[b][h]; all else is as above, positions and the window counted in what the head sees. */
 typedef struct fc_paged_attention {
   fc_tensor q;            /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
   fc_tensor k_cache;      /* [pages, P, Hk, D], in any order of strides with D innermost; rows 16-byte aligned */
   fc_tensor v_cache;
-  fc_tensor table;        /* i32 [B, W] */
-  fc_tensor lengths;      /* i32 [B] */
+  fc_tensor table;        /* i32 [B, W], or [B, Hk, W] */
+  fc_tensor lengths;      /* i32 [B], or [B, Hk] */
   fc_tensor out;          /* [B, Hq, D], out */
   fc_tensor lse;          /* f32 [B, Hq], out, or absent */
   double    scale;
   int32_t   window;
 } fc_paged_attention;
+
+/* Bounds of the keys of a page, for the pages that got new keys.  Request b has new keys at the positions max(lengths_before[b], 0) ..
+ * lengths[b]-1 (and below W P), which lie where fc_paged_attention finds them.  For each page that holds any, and each key head:
+ *   bounds[page][h][0] = the least, bounds[page][h][1] = the largest of every element of its new keys, and of what was there before where
+ *   the page's first position is below lengths_before[b].
+ * A NaN among the keys makes a NaN of both.  Pages outside the cache are left out; a page takes new keys of one request only.  Keys that a request drops from its end
+ * leave bounds that are still bounds.  A step that is run again gives the same.  Pages of a request that can have new keys times heads: 2^31-1 of all
+ * requests together (FC_E_LIMIT). */
+typedef struct fc_page_bounds {
+  fc_tensor k_cache;         /* [pages, P, Hk, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
+  fc_tensor table;           /* i32 [B, W] */
+  fc_tensor lengths_before;  /* i32 [B] */
+  fc_tensor lengths;         /* i32 [B] */
+  fc_tensor bounds;          /* [pages, Hk, 2, D] of the type of the cache, in and out; rows 16-byte aligned */
+} fc_page_bounds;
+
+/* The pages of a request that count most for each of its key heads.  Request b has pages(b) = min(ceil(lengths[b] / P), W) pages, P = page_size, its
+ * keys end at len = min(lengths[b], W P); an entry of the table that is no page of bounds is not there.  The score of a page for key head h
+ * bounds what any of its keys scores with a query head of the group:
+ *   s = max over the query heads of h of  sum over d of  max(q_d, 0) bounds[page][h][1][d] + min(q_d, 0) bounds[page][h][0][d]
+ * in 64 bits, a NaN counted as +inf.  Taken are the first `first` and the last `last` of the pages (1 and 1 keep what began the text and
+ * what is newest), and of the others those of the largest scores, of equal ones those that come first, S in all; all that are there where they are no more.
+ * selected[b][h]: their numbers in the order of the table, -1 behind them.  selected_lengths[b][h]: the keys they hold, which is P each but for
+ * the last page of the request.  Both are what fc_paged_attention takes as a table of rank 3 and its lengths.
+ * S P is at most 2^31-1, B Hk 2^24-1, B Hk times the pages of a request 2^36 (FC_E_LIMIT). */
+typedef struct fc_page_select {
+  fc_tensor q;                 /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
+  fc_tensor bounds;            /* [pages, Hk, 2, D] of the same type; rows 16-byte aligned */
+  fc_tensor table;             /* i32 [B, W] */
+  fc_tensor lengths;           /* i32 [B] */
+  fc_tensor selected;          /* i32 [B, Hk, S], out */
+  fc_tensor selected_lengths;  /* i32 [B, Hk], out */
+  int32_t   page_size;
+  int32_t   first;
+  int32_t   last;              /* first + last <= S */
+} fc_page_select;
+
+/* Attention of one new token of each request whose keys are those of a prefix, which all requests of a group share, and its own behind them.
+ * Group g: the requests group_start[g] .. group_start[g+1]-1, whose prefix are the prefix_lengths[g] keys on the pages prefix_table[g]; requests
+ * before group_start[0] and from group_start[G] on have no prefix.  A start below an earlier one counts as that one, below 0 as 0, above B as B.  Request
+ * b's own keys are the lengths[b] keys on the pages table[b].  The result is that of fc_paged_attention without a window over both, each key
+ * of a prefix read once for 32 to 128 of the query heads that see it.  A request may have no keys of its own, a group no prefix.
+ * At most 1024 groups; pieces of a prefix (32 keys of a key head for 128 query heads, at least) are counted in 31 bits, of as many keys as its
+ * table could hold (FC_E_LIMIT). */
+typedef struct fc_prefix_attention {
+  fc_tensor q;               /* as in fc_paged_attention */
+  fc_tensor k_cache;
+  fc_tensor v_cache;
+  fc_tensor prefix_table;    /* i32 [G, Wp] */
+  fc_tensor prefix_lengths;  /* i32 [G] */
+  fc_tensor group_start;     /* i32 [G + 1] */
+  fc_tensor table;           /* i32 [B, W] */
+  fc_tensor lengths;         /* i32 [B] */
+  fc_tensor out;             /* [B, Hq, D], out */
+  fc_tensor lse;             /* f32 [B, Hq], out, or absent */
+  double    scale;
+} fc_prefix_attention;
 
 /* Bytes of scratch a list of operators needs. */
 int fc_operators_scratch_bytes(const fc_operator *ops, int32_t n, size_t *bytes);

@@ -119,3 +119,100 @@ def paged_attention(q, k_cache, v_cache, table, lengths, scale, window=0):
             out[b, h], lse[b, h] = p @ v / p.sum(), top + np.log(p.sum())
             reach[b, h], spread[b, h] = abs(scale) * (np.abs(k) @ np.abs(q[b, h])).max(), p @ np.abs(v) / p.sum()
     return out, lse, reach, spread
+
+
+def page_bounds(k_cache, table, lengths_before, lengths, bounds):
+    """bounds [pages, H, 2, D] after a step."""
+    bounds = bounds.copy()
+    pages, page = k_cache.shape[:2]
+    for b in range(len(lengths)):
+        before = max(int(lengths_before[b]), 0)
+        of_page = {}
+        for j in range(before, min(int(lengths[b]), table.shape[1] * page)):
+            of_page.setdefault(j // page, []).append(j % page)
+        for w, places in of_page.items():
+            p = int(table[b, w])
+            if not 0 <= p < pages:
+                continue
+            keys = k_cache[p, places]                        # [new, H, D]
+            low, high = keys.min(0), keys.max(0)
+            if w * page < before:
+                low, high = np.minimum(low, bounds[p, :, 0]), np.maximum(high, bounds[p, :, 1])
+            bounds[p, :, 0], bounds[p, :, 1] = low, high
+    return bounds
+
+
+def page_scores(q, bounds):
+    """What bounds [n, 2, D] of pages let their keys score with the queries [group, D] of a key head."""
+    with np.errstate(invalid="ignore"):
+        s = np.array([[(np.maximum(x, 0) * high + np.minimum(x, 0) * low).sum() for x in q] for low, high in bounds])
+    return np.where(np.isnan(s), np.inf, s).max(1)
+
+
+def page_select(q, bounds, table, lengths, page, most, first, last):
+    """selected [B, H, most] and the keys selected pages hold [B, H]."""
+    batch, width = table.shape
+    pages, kv = bounds.shape[:2]
+    group = q.shape[1] // kv
+    selected, held = np.full((batch, kv, most), -1, np.int32), np.zeros((batch, kv), np.int32)
+    for b in range(batch):
+        keys = min(max(int(lengths[b]), 0), width * page)
+        count = -(-keys // page)
+        there = [w for w in range(count) if 0 <= table[b, w] < pages]
+        for h in range(kv):
+            taken = [w for w in there if w < first or w >= count - last]
+            if len(there) <= most:
+                taken = there
+            else:
+                rest = [w for w in there if w not in set(taken)]
+                s = page_scores(q[b, h * group:(h + 1) * group], bounds[table[b, rest], h])
+                taken = sorted(taken + [rest[i] for i in np.argsort(-s, kind="stable")[:most - len(taken)]])
+            selected[b, h, :len(taken)] = table[b, taken]
+            held[b, h] = sum(min(page, keys - w * page) for w in taken)
+    return selected, held
+
+
+def attention_of_heads(q, k_cache, v_cache, places, scale):
+    """paged_attention where places(b, h) lists the (page, place) that key head h of request b sees; pages outside the cache are left out."""
+    batch, heads, _ = q.shape
+    pages, _, kv, _ = k_cache.shape
+    out, lse = np.zeros(q.shape), np.full((batch, heads), -np.inf)
+    reach, spread = np.zeros((batch, heads)), np.zeros(q.shape)
+    for b in range(batch):
+        for n in range(kv):
+            at = np.array([(p, o) for p, o in places(b, n) if 0 <= p < pages], np.int64).reshape(-1, 2)
+            if not len(at):
+                continue
+            k, v = (cache[at[:, 0], at[:, 1], n] for cache in (k_cache, v_cache))
+            for h in range(n * (heads // kv), (n + 1) * (heads // kv)):
+                score = scale * (k @ q[b, h])
+                top = score.max()
+                if top == -np.inf:
+                    continue
+                p = np.exp(score - top)
+                out[b, h], lse[b, h] = p @ v / p.sum(), top + np.log(p.sum())
+                reach[b, h], spread[b, h] = abs(scale) * (np.abs(k) @ np.abs(q[b, h])).max(), p @ np.abs(v) / p.sum()
+    return out, lse, reach, spread
+
+
+def keys_on(pages, page, length):
+    """(page, place) of the first `length` keys on these pages, one after the other."""
+    return [(int(pages[j // page]), j % page) for j in range(min(max(int(length), 0), len(pages) * page))]
+
+
+def selected_attention(q, k_cache, v_cache, table, lengths, scale, window=0):
+    """table [B, H, W], lengths [B, H]."""
+    page = k_cache.shape[1]
+    cut = lambda b, h: max(0, int(lengths[b, h]) - window) if window else 0  # noqa: E731
+    return attention_of_heads(q, k_cache, v_cache, lambda b, h: keys_on(table[b, h], page, lengths[b, h])[cut(b, h):], scale)
+
+
+def prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lengths, group_start, table, lengths, scale):
+    page, batch = k_cache.shape[1], len(lengths)
+    start = np.maximum.accumulate(np.clip(group_start, 0, batch))
+    group = {b: g for g in range(len(prefix_lengths)) for b in range(start[g], start[g + 1])}
+
+    def places(b, h):
+        shared = keys_on(prefix_table[group[b]], page, prefix_lengths[group[b]]) if b in group else []
+        return shared + keys_on(table[b], page, lengths[b])
+    return attention_of_heads(q, k_cache, v_cache, places, scale)

@@ -134,6 +134,20 @@ class fc_paged_attention(C.Structure):
     _fields_ = _tensors("q", "k_cache", "v_cache", "table", "lengths", "out", "lse") + [("scale", C.c_double), ("window", C.c_int32)]
 
 
+class fc_page_bounds(C.Structure):
+    _fields_ = _tensors("k_cache", "table", "lengths_before", "lengths", "bounds")
+
+
+class fc_page_select(C.Structure):
+    _fields_ = _tensors("q", "bounds", "table", "lengths", "selected", "selected_lengths") + [("page_size", C.c_int32), ("first", C.c_int32),
+                                                                                              ("last", C.c_int32)]
+
+
+class fc_prefix_attention(C.Structure):
+    _fields_ = _tensors("q", "k_cache", "v_cache", "prefix_table", "prefix_lengths", "group_start", "table", "lengths", "out", "lse") + [
+        ("scale", C.c_double)]
+
+
 _lib = None
 
 
@@ -572,13 +586,47 @@ class HeadNormRopeGrad(CacheOperator):
 
 
 class PagedAttention(CacheOperator):
-    """Attention of one new token of each request over its pages: see fc_paged_attention.  scale None: 1 / sqrt(D)."""
+    """Attention of one new token of each request over its pages, or over those that each of its key heads has (a table of rank 3): see
+    fc_paged_attention.  scale None: 1 / sqrt(D)."""
 
     kind, struct = 3, fc_paged_attention
 
     def __init__(self, *, q, k_cache, v_cache, table, lengths, out, lse=None, scale: Optional[float] = None, window: int = 0):
         self._describe(dict(q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths, out=out, lse=lse),
                        scale=q.shape[-1] ** -0.5 if scale is None else scale, window=window)
+
+
+class PageBounds(CacheOperator):
+    """The least and the largest of every element of the keys of a page, for the pages with new keys: see fc_page_bounds."""
+
+    kind, struct = 4, fc_page_bounds
+
+    def __init__(self, *, k_cache, table, lengths_before, lengths, bounds):
+        self._describe(dict(k_cache=k_cache, table=table, lengths_before=lengths_before, lengths=lengths, bounds=bounds))
+
+
+class PageSelect(CacheOperator):
+    """The pages of a request that can count most for each of its key heads, by their bounds: see fc_page_select.  `selected` and
+    `selected_lengths` are what PagedAttention then takes for table and lengths."""
+
+    kind, struct = 5, fc_page_select
+
+    def __init__(self, *, q, bounds, table, lengths, page_size: int, selected, selected_lengths, first: int = 1, last: int = 1):
+        self._describe(dict(q=q, bounds=bounds, table=table, lengths=lengths, selected=selected, selected_lengths=selected_lengths),
+                       page_size=page_size, first=first, last=last)
+
+
+class PrefixAttention(CacheOperator):
+    """Attention of one new token of each request over the prefix that the requests of its group share and over its own pages behind it: see
+    fc_prefix_attention.  scale None: 1 / sqrt(D)."""
+
+    kind, struct = 6, fc_prefix_attention
+
+    def __init__(self, *, q, k_cache, v_cache, prefix_table, prefix_lengths, group_start, table, lengths, out, lse=None,
+                 scale: Optional[float] = None):
+        self._describe(dict(q=q, k_cache=k_cache, v_cache=v_cache, prefix_table=prefix_table, prefix_lengths=prefix_lengths,
+                            group_start=group_start, table=table, lengths=lengths, out=out, lse=lse),
+                       scale=q.shape[-1] ** -0.5 if scale is None else scale)
 
 
 def _operators(ops: Sequence[CacheOperator]):

@@ -22,7 +22,8 @@ LIB = os.path.join(HERE, "libfc.so")
 BOUND = os.path.join(HERE, "_bound_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["api.hip", "run.hip", "instances.hip", "interp.hip", "generic_folds.hip", "generic_rows.hip", "generic_scans.hip", "model.cpp",
-           "plan.cpp", "operators.hip", "page_map.hip", "head_norm_rope.hip", "paged_attention.hip"]
+           "plan.cpp", "operators.hip", "page_map.hip", "head_norm_rope.hip", "paged_attention.hip",
+           "attention_of_heads.hip", "attention_after_prefix.hip", "prefix_attention.hip", "page_bounds.hip", "page_select.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -89,6 +89,9 @@ int check_operators(const fc_operator *ops, int32_t n, OperatorList &out, std::s
       case FC_HEAD_NORM_ROPE: rc = make_head_norm_rope(*static_cast<const fc_head_norm_rope *>(ops[i].args), op, err); break;
       case FC_HEAD_NORM_ROPE_GRAD: rc = make_head_norm_rope_grad(*static_cast<const fc_head_norm_rope_grad *>(ops[i].args), op, err); break;
       case FC_PAGED_ATTENTION: rc = make_paged_attention(*static_cast<const fc_paged_attention *>(ops[i].args), op, err); break;
+      case FC_PAGE_BOUNDS: rc = make_page_bounds(*static_cast<const fc_page_bounds *>(ops[i].args), op, err); break;
+      case FC_PAGE_SELECT: rc = make_page_select(*static_cast<const fc_page_select *>(ops[i].args), op, err); break;
+      case FC_PREFIX_ATTENTION: rc = make_prefix_attention(*static_cast<const fc_prefix_attention *>(ops[i].args), op, err); break;
       default: err = "unknown kind " + std::to_string(ops[i].kind); rc = FC_E_ARG;
     }
     if (rc != FC_OK) { err = "operator " + std::to_string(i) + ": " + err; return rc; }

@@ -56,6 +56,9 @@ int make_page_map(const fc_page_map &a, std::unique_ptr<Operator> &out, std::str
 int make_head_norm_rope(const fc_head_norm_rope &a, std::unique_ptr<Operator> &out, std::string &err);
 int make_head_norm_rope_grad(const fc_head_norm_rope_grad &a, std::unique_ptr<Operator> &out, std::string &err);
 int make_paged_attention(const fc_paged_attention &a, std::unique_ptr<Operator> &out, std::string &err);
+int make_page_bounds(const fc_page_bounds &a, std::unique_ptr<Operator> &out, std::string &err);
+int make_page_select(const fc_page_select &a, std::unique_ptr<Operator> &out, std::string &err);
+int make_prefix_attention(const fc_prefix_attention &a, std::unique_ptr<Operator> &out, std::string &err);
 
 int check_operators(const fc_operator *ops, int32_t n, OperatorList &out, std::string &err);
 size_t operators_scratch_bytes(const OperatorList &list);
@@ -91,7 +94,7 @@ inline int size_of_dtype(int32_t dtype) { return dtype == FC_I64 ? 8 : dtype == 
 // the largest power of two, `most` at most, that the base and all strides but the innermost (in elements) are multiples of
 int common_alignment(const fc_tensor &t, int most);
 
-inline unsigned ceil_div(unsigned long long a, unsigned long long b) { return (unsigned)((a + b - 1) / b); }
+__host__ __device__ inline unsigned ceil_div(unsigned long long a, unsigned long long b) { return (unsigned)((a + b - 1) / b); }
 
 // ------------------------------------------------------------------ device
 template <class T, int N> using Vec = T __attribute__((ext_vector_type(N)));      // aligned to its size
