@@ -1,7 +1,7 @@
 // The pages of a request that count most for a key head (include/fc.h, fc_page_select).
 //
-// No key of a page scores more with q than  s = sum over d of max(q_d, 0) high_d + min(q_d, 0) low_d,  which is a matrix product: bounds of 16 pages
-// are its rows, the query heads of a group its columns.  Its sums are of 64 bits, as is the matrix instruction: which of two pages is taken must not
+// No key of a page scores more with q than  s = sum over d of max(q_d, 0) high_d + min(q_d, 0) low_d,  which is a matrix product: bounds of
+// pages are its rows, the query heads of a group its columns.  Its sums are of 64 bits, as is the matrix instruction: which of two pages is taken must not
 // depend on the order in which they were added up.  Of the s of a group's heads the largest counts.
 //
 // The scores become whole numbers of 64 bits in the same order; the k-th largest is found from its upper digits down, 8 bits at a time, from
@@ -16,7 +16,10 @@ namespace fc {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kColumns = 16;
+constexpr int kTilesOfWave = 1;                             // of 16 pages, that a wave reads before it scores them
+constexpr unsigned kBlockPages = 16 * kTilesOfWave * kWaves; // of a row that a workgroup scores at a time
+constexpr unsigned kKept = 1024;                             // keys that stay in LDS where one workgroup has a whole row
+constexpr unsigned kListed = 2048;                           // selected positions that are put in order in LDS
 constexpr unsigned long long kAlways = ~0ull;                // above every score; 0, below every score, is a page that is not there
 
 struct SelectArgs {
@@ -29,8 +32,6 @@ struct SelectArgs {
   unsigned requests, heads, group, dim, page, pages, width, most, first, last, parts;
 };
 
-using Acc64 = Vec<double, 4>;
-
 // a number that orders scores as they are; NaN counts as infinite, -0 as 0
 __device__ __forceinline__ unsigned long long key_of(double s) {
   s = s != s ? __builtin_inf() : s + 0.0;
@@ -38,83 +39,125 @@ __device__ __forceinline__ unsigned long long key_of(double s) {
   return bits >> 63 ? ~bits : bits | 1ull << 63;
 }
 
-// the largest over the 16 lanes of a row
-__device__ __forceinline__ double row_max(double v) {
-#pragma unroll
-  for (int s = 1; s < 16; s *= 2) v = fmax(v, __shfl_xor(v, s));
-  return v;
+// the value of another lane of the four
+template <int Ctrl> __device__ __forceinline__ double of_four(double v) {
+  const unsigned long long bits = __builtin_bit_cast(unsigned long long, v);
+  const unsigned low = (unsigned)dpp_move<Ctrl>(0, (int)(unsigned)bits), high = (unsigned)dpp_move<Ctrl>(0, (int)(unsigned)(bits >> 32));
+  return __builtin_bit_cast(double, (unsigned long long)high << 32 | low);
 }
 
-// Scores of the 16 kTiles pages from `at` on of the row's `count`, use(position, key).
-template <class T, int Tiles, class Use>
-__device__ __forceinline__ void score(const SelectArgs &a, const T *q, const T *bounds, const int *table, unsigned at, unsigned count, Use &&use) {
-  constexpr int N = 16 / sizeof(T);
-  const unsigned r = lane_id() & 15, g = lane_id() >> 4;
-  const T *low[Tiles];
-  bool there[Tiles];
+// Scores of pages for the query heads of a key head.  The instruction has four products of 4 pages, 4 elements and 4 heads: lane (r, g), r = lane % 16,
+// g = lane / 16, holds elements of page r, and of query head r % 4 the same ones; lane (4 n + j, i) gets page 4 n + i and head j.
+// HeadTiles: four query heads each that are taken together.  Whole: the elements of a head fill the lanes' reads.
+template <class T, int HeadTiles, bool Whole> struct Scores {
+  static constexpr int N = 16 / sizeof(T), kChunks = 4, kTiles = kTilesOfWave;  // 16 bytes of each of four lanes; of them, and of 16 pages, under way
+  using Part = Vec<T, N>;
+  const SelectArgs &a;
+  const T *q, *bounds;
+  const int *table;
+  unsigned r, g;
+
+  __device__ __forceinline__ Scores(const SelectArgs &args, const T *queries, const T *of_head, const int *pages)
+      : a(args), q(queries), bounds(of_head), table(pages), r(lane_id() & 15), g(lane_id() >> 4) {}
+
+  // all reads are made, so that none waits for a condition: past the end of a head they are of its last elements, and then cleared
+  static __device__ __forceinline__ Part load(const T *from, unsigned d, unsigned dim) { return load_vec<T, N>(from + (Whole ? d : min(d, dim - N))); }
+  static __device__ __forceinline__ void clear(Part &x, bool inside) {
+    if constexpr (!Whole)
 #pragma unroll
-  for (int t = 0; t < Tiles; ++t) {
-    const unsigned w = at + 16 * t + r;
-    const unsigned page = w < count ? (unsigned)table[w] : a.pages;
-    there[t] = page < a.pages;
-    low[t] = bounds + (there[t] ? page * a.b_page : 0ll);
+      for (int e = 0; e < N; ++e) x[e] = inside ? x[e] : (T)0.0f;
   }
-  double best[Tiles][4];
+
+  // use(position, is it there, score, is it the first) for the 16 kTiles pages from `at` on that lie below `end`, for every 4 HeadTiles query heads
+  template <class Use> __device__ __forceinline__ void run(unsigned at, unsigned end, Use &&use) {
+    if (at >= end) return;
+    const T *row[kTiles];
+    unsigned long long there[kTiles];
 #pragma unroll
-  for (int t = 0; t < Tiles; ++t)
+    for (int t = 0; t < kTiles; ++t) {
+      const unsigned w = at + 16 * t + r, page = (unsigned)table[min(w, end - 1)];
+      const bool is_there = w < end && page < a.pages;
+      there[t] = __ballot(is_there);
+      row[t] = bounds + (is_there ? page * a.b_page : 0ll);
+    }
+    for (unsigned head0 = 0; head0 < a.group; head0 += 4 * HeadTiles) {
+      const T *from[HeadTiles];
+      bool mine[HeadTiles], nan[HeadTiles];
+      double up[kTiles][HeadTiles], down[kTiles][HeadTiles];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) best[t][i] = -__builtin_inf();
-  for (unsigned head0 = 0; head0 < a.group; head0 += kColumns) {
-    Acc64 sums[Tiles];
+      for (int n = 0; n < HeadTiles; ++n) {
+        const unsigned head = head0 + 4 * n + (r & 3);
+        mine[n] = head < a.group;
+        from[n] = q + (mine[n] ? head * a.q_head : 0ll);
+        nan[n] = false;
 #pragma unroll
-    for (int t = 0; t < Tiles; ++t) sums[t] = Acc64{0.0, 0.0, 0.0, 0.0};
-    const bool mine = head0 + r < a.group;
-    const T *const from = q + (mine ? (head0 + r) * a.q_head : 0ll);
-    for (unsigned d0 = 0; d0 < a.dim; d0 += 4 * N) {
-      const unsigned d = d0 + g * N;
-      const bool inside = d < a.dim;
-      Vec<T, N> x, l[Tiles], h[Tiles];
+        for (int t = 0; t < kTiles; ++t) up[t][n] = down[t][n] = 0.0;
+      }
+      for (unsigned d0 = g * N; d0 < a.dim + g * N; d0 += 4 * N * kChunks) {
+        Part x[HeadTiles][kChunks], l[kTiles][kChunks], h[kTiles][kChunks];
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = (T)0.0f;
-      if (mine && inside) x = load_vec<T, N>(from + d);
+        for (int c = 0; c < kChunks; ++c) {
+          const unsigned d = d0 + 4 * N * c;
+          if (d - g * N >= a.dim) break;                     // the same for all lanes
 #pragma unroll
-      for (int t = 0; t < Tiles; ++t) {
+          for (int n = 0; n < HeadTiles; ++n) x[n][c] = load(from[n], d, a.dim);
 #pragma unroll
-        for (int e = 0; e < N; ++e) l[t][e] = h[t][e] = (T)0.0f;
-        if (there[t] && inside) {
-          l[t] = load_vec<T, N>(low[t] + d);
-          h[t] = load_vec<T, N>(low[t] + a.b_half + d);
+          for (int t = 0; t < kTiles; ++t) {
+            h[t][c] = load(row[t] + a.b_half, d, a.dim);
+            l[t][c] = load(row[t], d, a.dim);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          const unsigned d = d0 + 4 * N * c;
+          if (d - g * N >= a.dim) break;
+#pragma unroll
+          for (int n = 0; n < HeadTiles; ++n) clear(x[n][c], d < a.dim);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            clear(h[t][c], d < a.dim);
+            clear(l[t][c], d < a.dim);
+          }
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            double high[kTiles], low[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+              high[t] = (double)(float)h[t][c][e];
+              low[t] = (double)(float)l[t][c][e];
+            }
+#pragma unroll
+            for (int n = 0; n < HeadTiles; ++n) {
+              const float v = (float)x[n][c][e];
+              nan[n] |= v != v;                              // which the maxima and minima would lose
+              const double plus = (double)fmaxf(v, 0.0f), minus = (double)fminf(v, 0.0f);
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t) {
+                up[t][n] = __builtin_amdgcn_mfma_f64_4x4x4f64(high[t], plus, up[t][n], 0, 0, 0);
+                down[t][n] = __builtin_amdgcn_mfma_f64_4x4x4f64(low[t], minus, down[t][n], 0, 0, 0);
+              }
+            }
+          }
         }
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float v = (float)x[e];
-        // a NaN goes into both
-        const double up = (double)(v < 0.0f ? 0.0f : v), down = (double)(v > 0.0f ? 0.0f : v);
+      for (int n = 0; n < HeadTiles; ++n) nan[n] = (__ballot(nan[n]) & (0x1111111111111111ull << (r & 3))) != 0;       // of all lanes of the head
 #pragma unroll
-        for (int t = 0; t < Tiles; ++t) {
-          sums[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(float)h[t][e], up, sums[t], 0, 0, 0);
-          sums[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(float)l[t][e], down, sums[t], 0, 0, 0);
+      for (int t = 0; t < kTiles; ++t) {
+        double best = -__builtin_inf();
+#pragma unroll
+        for (int n = 0; n < HeadTiles; ++n) {
+          const double s = up[t][n] + down[t][n];
+          if (mine[n]) best = fmax(best, s != s || nan[n] ? __builtin_inf() : s);
         }
+        best = fmax(best, of_four<0xb1>(best));              // quad_perm 1,0,3,2
+        best = fmax(best, of_four<0x4e>(best));              // quad_perm 2,3,0,1
+        const unsigned i = (r >> 2) * 4 + g, w = at + 16 * t + i;
+        if ((r & 3) == 0 && w < end) use(w, (there[t] >> i & 1) != 0, best, head0 == 0);
       }
     }
-    if (mine)
-#pragma unroll
-      for (int t = 0; t < Tiles; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) best[t][i] = fmax(best[t][i], sums[t][i] != sums[t][i] ? __builtin_inf() : sums[t][i]);
   }
-  // row i of the product's four in this lane: page 4 i + g
-#pragma unroll
-  for (int t = 0; t < Tiles; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double s = row_max(best[t][i]);
-      const unsigned w = at + 16 * t + 4 * i + g;
-      const bool is_there = __shfl((int)there[t], 4 * i + (int)g) != 0;
-      if (r == 0 && w < count) use(w, !is_there ? 0ull : w < a.first || w + a.last >= count ? kAlways : key_of(s));
-    }
-}
+};
 
 // Adds this workgroup to `counter`, once what it has stored has arrived; true for the last of `all`.
 __device__ __forceinline__ bool last_to_arrive(unsigned *counter, unsigned all) {
@@ -129,162 +172,232 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, unsigned all) 
   return before == all - 1;
 }
 
-// The sum over the workgroup up to this thread; total comes back too.  `lds`: kWaves words.
-__device__ __forceinline__ unsigned sum_up_to(unsigned v, unsigned *lds, unsigned &total) {
-  const unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)v);
+// The sums of two numbers over the workgroup up to this thread, and in all.
+struct Sums {
+  unsigned x, y, all_x, all_y;
+};
+__device__ __forceinline__ Sums sum_up_to(unsigned x, unsigned y, unsigned (*lds)[2]) {
+  const unsigned to_x = (unsigned)wave_scan_inclusive<AddI32>((int)x), to_y = (unsigned)wave_scan_inclusive<AddI32>((int)y);
+  if (lane_id() == kWave - 1) { lds[wave_id()][0] = to_x; lds[wave_id()][1] = to_y; }
   __syncthreads();
-  if (lane_id() == kWave - 1) lds[wave_id()] = upto;
-  __syncthreads();
-  unsigned before = 0;
-  total = 0;
+  Sums s{to_x, to_y, 0, 0};
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave_id()) before += lds[w];
-    total += lds[w];
+    if (w < wave_id()) { s.x += lds[w][0]; s.y += lds[w][1]; }
+    s.all_x += lds[w][0];
+    s.all_y += lds[w][1];
   }
-  return before + upto;
+  return s;
 }
 
-// Kept: keys in LDS
-template <class T, int Kept> __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
-  constexpr int kTiles = 4;
-  __shared__ unsigned long long kept[Kept];
-  __shared__ unsigned counts[256], sums[kWaves], found[2];
-  __shared__ unsigned long long ends[2][kWaves];
+// keys of a row in memory
+__device__ __host__ __forceinline__ size_t far_keys(unsigned width) { return ((size_t)width + kThreads - 1) / kThreads * kThreads; }
+
+// Held: keys of a row that a thread keeps in registers, side by side; 0: as many as there are, read again whenever they are looked at
+template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+  __shared__ unsigned long long kept[kKept];
+  __shared__ unsigned counts[2][256], sums[2][kWaves][2], found[2][3];
+  __shared__ int ends[2][kWaves];
+  __shared__ unsigned listed[kListed];
   const unsigned row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   const unsigned b = row / a.heads, head = row - b * a.heads;
-  const unsigned keys = (unsigned)min((unsigned long long)max(load_scalar(a.lengths + b), 0), (unsigned long long)a.width * a.page);
-  const unsigned count = (keys + a.page - 1) / a.page;
+  const unsigned length = (unsigned)min((unsigned long long)max(load_scalar(a.lengths + b), 0), (unsigned long long)a.width * a.page);
+  const unsigned count = (length + a.page - 1) / a.page;
   const int *const table = a.table + b * a.table_stride;
   int *const selected = a.selected + b * a.s_request + head * a.s_head;
-  unsigned long long *const far = a.keys ? a.keys + (size_t)row * a.width : nullptr;
-  const bool near = a.parts == 1 && count <= (unsigned)Kept;                   // the keys never leave LDS
-  {
+  unsigned long long *const far = a.keys ? a.keys + (size_t)row * far_keys(a.width) : nullptr;
+  const bool scored = count > a.most && a.pages > 0;                        // else all that are there are taken
+  const unsigned parts = scored ? min(a.parts, (count + kBlockPages - 1) / kBlockPages) : 1u;
+  if (part >= parts) return;
+  const bool near = parts == 1 && count <= kKept;            // the keys never leave LDS
+  // each thread has positions of its own, side by side; in memory their keys lie so that a wave reads neighbours
+  const unsigned each = (count + kThreads - 1) / kThreads, w0 = min(threadIdx.x * each, count), w1 = min(w0 + each, count);
+  if (scored) {
     const T *const q = reinterpret_cast<const T *>(a.q) + b * a.q_request + head * a.group * a.q_head;
     const T *const bounds = reinterpret_cast<const T *>(a.bounds) + head * a.b_head;
-    const unsigned step = 16 * kTiles * kWaves * a.parts;
-    for (unsigned at = (part * kWaves + (unsigned)wave_id()) * 16 * kTiles; at < count; at += step)
-      score<T, kTiles>(a, q, bounds, table, at, count, [&](unsigned w, unsigned long long key) {
-        if (near) kept[w] = key;
-        else store_agent64(far + w, key);
+    Scores<T, HeadTiles, Whole> scores(a, q, bounds, table);
+    for (unsigned at = part * kBlockPages; at < count; at += parts * kBlockPages)
+      scores.run(at + kBlockPages / kWaves * (unsigned)wave_id(), min(at + kBlockPages, count), [&](unsigned w, bool there, double s, bool first) {
+        unsigned long long key = !there ? 0ull : w < a.first || w + a.last >= count ? kAlways : key_of(s);
+        if (near) kept[w] = first ? key : max(kept[w], key);
+        else {
+          unsigned long long *const to = far + w / each + (size_t)(w % each) * kThreads;
+          store_agent64(to, first ? key : max(load_agent64(to), key));
+        }
       });
   }
-  if (a.parts > 1 && !last_to_arrive(a.counters + row, a.parts)) return;
-  if (!near) {
+  if (parts > 1) {
+    if (!last_to_arrive(a.counters + row, parts)) return;
+  } else {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    for (unsigned w = threadIdx.x; w < min(count, (unsigned)Kept); w += kThreads) kept[w] = load_agent64(far + w);
   }
-  __syncthreads();
-  auto key_at = [&](unsigned w) { return w < (unsigned)Kept ? kept[w] : load_agent64(far + w); };
-
-  // the least and the largest score, and how many pages there are
-  unsigned long long least = kAlways, largest = 0;
-  unsigned mine = 0, always = 0;
-  for (unsigned w = threadIdx.x; w < count; w += kThreads) {
-    const unsigned long long key = key_at(w);
-    mine += key != 0;
-    always += key == kAlways;
-    if (key != 0 && key != kAlways) {
-      least = min(least, key);
-      largest = max(largest, key);
-    }
-  }
-  unsigned candidates, wanted;
-  sum_up_to(mine, sums, candidates);
-  sum_up_to(always, sums, wanted);
-  wanted = a.most - min(wanted, a.most);                                       // of those that are not taken anyway
-  // taken: keys above `bar` with their lowest `shift` bits cut off, and of those at it the first `level`
-  unsigned long long bar = 0;
-  unsigned shift = 0, level = ~0u;
-  if (candidates > a.most && wanted == 0) bar = ~0ull, level = 0;
-  else if (candidates > a.most) {
+  // N keys from the thread's i0-th on, all read before the first is waited for; 0 behind its last
+  auto read_keys = [&](unsigned i0, auto &to) {
+    constexpr int n = sizeof(to) / sizeof(to[0]);
+    if (!scored) {
+      unsigned page[n];
 #pragma unroll
-    for (int s = 1; s < kWave; s *= 2) {
-      least = min(least, (unsigned long long)__shfl_xor((long long)least, s));
-      largest = max(largest, (unsigned long long)__shfl_xor((long long)largest, s));
-    }
-    if (lane_id() == 0) { ends[0][wave_id()] = least; ends[1][wave_id()] = largest; }
-    __syncthreads();
+      for (int i = 0; i < n; ++i)
+        if (i0 + i < each) page[i] = (unsigned)table[min(w0 + i0 + i, count - 1)];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) { least = min(least, ends[0][w]); largest = max(largest, ends[1][w]); }
-    unsigned bits = least == largest ? 0u : 64u - (unsigned)__clzll((long long)(least ^ largest));   // below which keys differ
-    bar = bits == 64 ? 0 : largest >> bits;
-    shift = bits;
-    level = wanted;
-    while (shift > 0) {
-      const unsigned digit = min(shift, 8u);
-      shift -= digit;
-      __syncthreads();
-      counts[threadIdx.x] = 0;
-      __syncthreads();
-      for (unsigned w = threadIdx.x; w < count; w += kThreads) {
-        const unsigned long long key = key_at(w);
-        if (key != 0 && key != kAlways && (shift + digit == 64 ? 0 : key >> (shift + digit)) == bar) atomicAdd(&counts[key >> shift & ((1u << digit) - 1)], 1u);
+      for (int i = 0; i < n; ++i) to[i] = w0 + i0 + i < w1 && page[i] < a.pages ? kAlways : 0ull;
+    } else {
+      if (near)
+#pragma unroll
+        for (int i = 0; i < n; ++i) to[i] = kept[min(w0 + i0 + i, count - 1)];
+      else
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+          if (i0 + i < each) to[i] = load_agent64(far + threadIdx.x + (size_t)(i0 + i) * kThreads);
+#pragma unroll
+      for (int i = 0; i < n; ++i) to[i] = w0 + i0 + i < w1 ? to[i] : 0ull;
+    }
+  };
+  unsigned long long held[Held ? Held : 1];
+  if constexpr (Held > 0) read_keys(0, held);
+  auto for_keys = [&](auto &&use) {
+    if constexpr (Held > 0) {
+#pragma unroll
+      for (int i = 0; i < Held; ++i)
+        if (held[i] != 0) use(w0 + i, held[i]);
+    } else {
+      for (unsigned i0 = 0; i0 < each; i0 += 8) {
+        unsigned long long some[8];
+        read_keys(i0, some);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (some[i] != 0) use(w0 + i0 + i, some[i]);
       }
-      __syncthreads();
-      // from the largest digit down: the one where `level` is reached
-      const unsigned d = 255u - threadIdx.x, here = counts[d];
-      unsigned total;
-      const unsigned upto = sum_up_to(here, sums, total);
-      if (level > upto - here && level <= upto) { found[0] = d; found[1] = upto - here; }
-      __syncthreads();
-      bar = bar << digit | found[0];
-      level -= found[1];
-      if (level == counts[found[0]]) break;                                    // all of them are taken
+    }
+  };
+
+  // taken: keys above `bar` with their lowest `shift` bits cut off, and of those at it the first `level`
+  unsigned long long bar = ~0ull;
+  unsigned shift = 0, level = 0, turn = 0;
+  bool all = true;
+  if (scored) {
+    // the upper halves of the keys, as signed numbers in the same order: the least, turned round, and the largest
+    int least = INT32_MIN, largest = INT32_MIN;
+    unsigned mine = 0, always = 0;
+    for_keys([&](unsigned, unsigned long long key) {
+      ++mine;
+      always += key == kAlways;
+      if (key != kAlways) {
+        const int upper = (int)((unsigned)(key >> 32) ^ 0x80000000u);
+        least = max(least, ~upper);
+        largest = max(largest, upper);
+      }
+    });
+    least = wave_reduce<MaxI32>(least);
+    largest = wave_reduce<MaxI32>(largest);
+    if (lane_id() == 0) { ends[0][wave_id()] = least; ends[1][wave_id()] = largest; }
+    counts[0][threadIdx.x] = 0;
+    const Sums there = sum_up_to(mine, always, sums[turn]);
+    turn ^= 1;
+    all = there.all_x <= a.most;
+    const unsigned wanted = a.most - min(there.all_y, a.most);                 // of those that are not taken anyway
+    if (!all && wanted > 0) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) { least = max(least, ends[0][w]); largest = max(largest, ends[1][w]); }
+      const unsigned upper = (unsigned)largest ^ 0x80000000u, differ = (unsigned)(~least ^ largest);
+      shift = differ ? 64u - (unsigned)__clz((int)differ) : 32u;               // keys differ below
+      bar = shift == 64 ? 0 : (unsigned long long)upper << 32 >> shift;
+      level = wanted;
+      for (unsigned n = 0; shift > 0; n ^= 1) {
+        const unsigned digit = min(shift, 8u), upper = shift;
+        shift -= digit;
+        for_keys([&](unsigned, unsigned long long key) {
+          if (key != kAlways && (upper == 64 ? 0 : key >> upper) == bar) atomicAdd(&counts[n][key >> shift & ((1u << digit) - 1)], 1u);
+        });
+        __syncthreads();
+        if (wave_id() == 0) {                                                  // from the largest digit down: the one where `level` is reached
+          unsigned here[4], mine4 = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine4 += here[i] = counts[n][255 - (4 * lane_id() + i)];
+          unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)mine4) - mine4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (level > upto && level <= upto + here[i]) {
+              found[n][0] = 255 - (4 * lane_id() + i);
+              found[n][1] = upto;
+              found[n][2] = here[i];
+            }
+            upto += here[i];
+          }
+        } else if (wave_id() == 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) counts[n ^ 1][4 * lane_id() + i] = 0;
+        }
+        __syncthreads();
+        bar = bar << digit | found[n][0];
+        level -= found[n][1];
+        if (level == found[n][2]) break;                                       // all of them are taken
+      }
     }
   }
-  // in order: each thread has positions of its own, side by side
-  const unsigned each = (count + kThreads - 1) / kThreads, w0 = min(threadIdx.x * each, count), w1 = min(w0 + each, count);
   unsigned above = 0, at_bar = 0;
-  for (unsigned w = w0; w < w1; ++w) {
-    const unsigned long long key = key_at(w);
-    if (key == 0) continue;
+  for_keys([&](unsigned, unsigned long long key) {
     const unsigned long long cut = key >> shift;
-    above += candidates <= a.most || key == kAlways || cut > bar;
-    at_bar += candidates > a.most && key != kAlways && cut == bar;
-  }
-  unsigned all_above, all_at;
-  const unsigned above_to = sum_up_to(above, sums, all_above), at_to = sum_up_to(at_bar, sums, all_at);
-  unsigned level_before = at_to - at_bar, slot = above_to - above + min(level_before, level);
-  const unsigned taken = min(all_above + min(all_at, level), a.most);
+    const bool over = all || key == kAlways || cut > bar;
+    above += over;
+    at_bar += !over && cut == bar;
+  });
+  const Sums to = sum_up_to(above, at_bar, sums[turn]);
+  unsigned at_before = to.y - at_bar, slot = to.x - above + min(at_before, level);
+  const unsigned taken = min(to.all_x + min(to.all_y, level), a.most);
   bool is_last = false;
-  for (unsigned w = w0; w < w1; ++w) {
-    const unsigned long long key = key_at(w);
-    if (key == 0) continue;
+  for_keys([&](unsigned w, unsigned long long key) {
     const unsigned long long cut = key >> shift;
-    bool take = candidates <= a.most || key == kAlways || cut > bar;
-    if (!take && cut == bar) take = level_before++ < level;
+    bool take = all || key == kAlways || cut > bar;
+    if (!take && cut == bar) take = at_before++ < level;
     if (take && slot < a.most) {
-      selected[slot++] = table[w];
+      if (slot < kListed) listed[slot] = w;
+      else selected[slot] = table[w];
+      ++slot;
       is_last |= w + 1 == count;
     }
-  }
+  });
+  const unsigned short_of = __syncthreads_or(is_last) ? count * a.page - length : 0u;
+  for (unsigned k = threadIdx.x; k < min(taken, kListed); k += kThreads) selected[k] = table[listed[k]];
   for (unsigned k = taken + threadIdx.x; k < a.most; k += kThreads) selected[k] = -1;
-  const unsigned short_of = __syncthreads_or(is_last) ? count * a.page - keys : 0u;
   if (threadIdx.x == 0) a.selected_lengths[b * a.l_request + head] = (int)(taken * a.page - short_of);
 }
 
-constexpr int kFew = 2048, kMany = 8192;
+// workgroups of a call: more rows than these have one each
+constexpr unsigned kWorkgroups = 2048;
 
 struct PageSelect final : Operator {
   SelectArgs a{};
   int32_t dtype;
-  bool many = false;                       // keys: more than kFew a row, or rows in parts
+  bool far = false;                        // keys leave LDS
   template <class F> void with_kernel(F &&f) const {
-    auto by = [&](auto t) {
+    auto by_width = [&](auto t, auto tiles, auto whole) {
       using T = decltype(t);
-      f(many ? &select_kernel<T, kMany> : &select_kernel<T, kFew>);
+      constexpr int kTiles = decltype(tiles)::value;
+      constexpr bool kWhole = decltype(whole)::value;
+      if (a.width <= 4 * kThreads) f(&select_kernel<T, kTiles, kWhole, 4>);
+      else if (a.width <= 8 * kThreads) f(&select_kernel<T, kTiles, kWhole, 8>);
+      else if (a.width <= 32 * kThreads) f(&select_kernel<T, kTiles, kWhole, 32>);
+      else f(&select_kernel<T, kTiles, kWhole, 0>);
     };
-    if (dtype == FC_F32) by(float{});
-    else if (dtype == FC_F16) by(_Float16{});
-    else by(__bf16{});
+    auto by_dim = [&](auto t, auto tiles) {
+      if (a.dim % (64 / sizeof(t)) == 0) by_width(t, tiles, std::true_type{});
+      else by_width(t, tiles, std::false_type{});
+    };
+    auto by_group = [&](auto t) {
+      if (a.group <= 4) by_dim(t, std::integral_constant<int, 1>{});
+      else by_dim(t, std::integral_constant<int, 2>{});
+    };
+    if (dtype == FC_F32) by_group(float{});
+    else if (dtype == FC_F16) by_group(_Float16{});
+    else by_group(__bf16{});
   }
-  size_t workspace() const override { return many ? (size_t)a.requests * a.heads * a.width * sizeof(unsigned long long) : 0; }
+  size_t workspace() const override { return far ? (size_t)a.requests * a.heads * far_keys(a.width) * sizeof(unsigned long long) : 0; }
   void record(Recorder &r) const override {
     if (a.requests == 0 || a.heads == 0) return;
     SelectArgs args = a;
-    args.keys = many ? reinterpret_cast<unsigned long long *>(r.workspace) : nullptr;
+    args.keys = far ? reinterpret_cast<unsigned long long *>(r.workspace) : nullptr;
     args.counters = r.counters;
     with_kernel([&](auto kernel) { r.launch(kernel, a.requests * a.heads * a.parts, kThreads, args); });
   }
@@ -308,7 +421,7 @@ int make_page_select(const fc_page_select &n, std::unique_ptr<Operator> &out, st
   if (!c.ok()) return c.code();
   const int64_t most = n.selected.shape[2], width = n.table.shape[1];
   if (n.page_size < 1) return c.fail(FC_E_ARG, "page_size must be positive").code();
-  if (kv < 1 || heads % kv) return c.fail(FC_E_ARG, "the heads of q must be a multiple of those of the bounds").code();
+  if (kv < 1 || heads < 1 || heads % kv) return c.fail(FC_E_ARG, "the heads of q must be a multiple of those of the bounds").code();
   if (dim < 8 || dim % 8 || dim > 256) return c.fail(FC_E_UNSUPPORTED, "heads have a multiple of 8 elements, at most 256").code();
   if (n.first < 0 || n.last < 0 || (int64_t)n.first + n.last > most) return c.fail(FC_E_ARG, "first and last must be positive and no more than are selected together").code();
   if (most * n.page_size > 0x7fffffff) return c.fail(FC_E_LIMIT, "the selected pages hold more than 2^31-1 keys").code();
@@ -346,8 +459,8 @@ int make_page_select(const fc_page_select &n, std::unique_ptr<Operator> &out, st
   // no more than the pages of a request of 2^31-1 keys are looked at
   a.width = (unsigned)std::min<uint64_t>(width, (0x7fffffffu + (uint64_t)a.page - 1) / a.page);
   const unsigned rows = a.requests * a.heads;
-  a.parts = rows ? std::max(1u, std::min(1024u / rows, ceil_div(a.width, 64 * kWaves))) : 1u;
-  op->many = a.width > (unsigned)kFew || a.parts > 1;
+  a.parts = rows && rows <= (unsigned)kCounters ? std::max(1u, std::min(kWorkgroups / rows, ceil_div(a.width, kBlockPages))) : 1u;
+  op->far = a.width > kKept || a.parts > 1;
   if ((uint64_t)rows * a.width > (uint64_t)1 << 36) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
   out = std::move(op);
   return FC_OK;

@@ -77,6 +77,7 @@ REFUSED = [
     ("FC_E_ARG", lambda: select(dtype="int32")),
     ("FC_E_ARG", lambda: select(hq=5)),
     ("FC_E_ARG", lambda: select(hk=0)),
+    ("FC_E_ARG", lambda: select(hq=0)),
     ("FC_E_ARG", lambda: select(bounds=T("float32", 9, 2, 2, 64))),
     ("FC_E_ARG", lambda: select(bounds=T("bfloat16", 9, 2, 2, 32))),
     ("FC_E_ARG", lambda: select(table=T("int32", 2, 8))),
