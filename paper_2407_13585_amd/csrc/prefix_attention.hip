@@ -8,6 +8,7 @@
 #include "attention.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace fc {
 
@@ -86,9 +87,9 @@ template <int Columns, int Tile> __device__ __forceinline__ void make_plan(const
   __syncthreads();
 }
 
-// Where a key lies; page a.pages: nowhere
+// Where a key and its value lie, in elements from the first of their key head
 struct Key {
-  unsigned page, place;
+  long long k, v;
 };
 
 template <class T, int Dim, int ColumnWaves> struct PrefixShape {
@@ -99,7 +100,8 @@ template <class T, int Dim, int ColumnWaves> struct PrefixShape {
   static constexpr int kLoads = kTile * kRow / kThreads;                     // of K, and of V, of a thread
   static constexpr size_t kTileBytes = 2 * (size_t)kTile * Dim * sizeof(T);
   static constexpr size_t kJoinBytes = (size_t)(kWaves - ColumnWaves) * (kTiles * Dim / 4 + 4) * kWave * sizeof(float);
-  static constexpr size_t kBytes = kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes;
+  static constexpr size_t kRowsBytes = (size_t)ColumnWaves * 16 * (Dim + 4) * sizeof(float);
+  static constexpr size_t kBytes = std::max({kTileBytes, kJoinBytes, kRowsBytes});
 };
 
 // where 16 bytes of a key's row lie in LDS: rows that are read side by side start at different banks
@@ -109,7 +111,7 @@ template <int Row> __device__ __forceinline__ unsigned place_in_lds(unsigned key
 }
 
 template <class T, int Dim, int ColumnWaves>
-__global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim == 128) ? 1 : 2) void prefix_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves == 1 || sizeof(T) == 4)) ? 1 : 2) void prefix_kernel(PrefixArgs a) {
   using S = PrefixShape<T, Dim, ColumnWaves>;
   constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = S::kWide, kChunks = Dim / (4 * kWide), kRow = S::kRow;
   constexpr int kW = Dim / 16, kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;
@@ -144,6 +146,9 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
   const unsigned r = lane_id() & 15, g4 = lane_id() >> 4;
   const unsigned wave = uniform((unsigned)wave_id()), column_wave = wave % ColumnWaves, key_wave = wave / ColumnWaves;
   const T *const q0 = reinterpret_cast<const T *>(a.q);
+  // 16 bits: what takes a product of q and k to the power of 2 that its weight is; m is such a power until the piece is written
+  const float by = sizeof(T) == 4 ? 1.0f : a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
+  auto power = [](float x) { return sizeof(T) == 4 ? exp_of(x) : __builtin_amdgcn_exp2f(x); };
   unsigned at = (unsigned)min((unsigned long long)blockIdx.x * share, (unsigned long long)total);
   const unsigned end = min(at + share, total);
   while (at < end) {
@@ -154,7 +159,9 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
     const unsigned kv = row / blocks, column0 = (row - kv * blocks) * S::kColumns + column_wave * 16 * kTiles;
     const unsigned columns = members * a.group;
     const int *const table = a.table + g * a.table_stride;
-    const T *const k0 = reinterpret_cast<const T *>(a.k) + kv * a.k_head, *const v0 = reinterpret_cast<const T *>(a.v) + kv * a.v_head;
+    const unsigned chunk = threadIdx.x % kRow, key0 = threadIdx.x / kRow;
+    const T *const k0 = reinterpret_cast<const T *>(a.k) + kv * a.k_head + min(chunk * kWide, a.dim - kWide);
+    const T *const v0 = reinterpret_cast<const T *>(a.v) + kv * a.v_head + min(chunk * kWide, a.dim - kWide);
     Frag q[kTiles][kChunks];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -168,6 +175,10 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
 #pragma unroll
         for (int i = 0; i < kWide; ++i) f[i] = (T)0.0f;
         if (column < columns && d < a.dim) f = load_vec<T, kWide>(from + d);
+        if constexpr (sizeof(T) == 2)                        // scores are then multiplied by a number above 0
+          if (!(a.scale > 0.0f))
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) f[i] = a.scale < 0.0f ? -f[i] : f[i] * (T)0.0f;
         q[t][c] = f;
       }
     }
@@ -181,55 +192,68 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
       for (int j = 0; j < kW; ++j) o[t][j] = Acc{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // where the keys of a unit lie: a thread for each
-    auto look_up = [&](unsigned unit) {
-      if (threadIdx.x < (unsigned)((S::kTile + kWave - 1) / kWave * kWave)) {
-        const unsigned j = unit * S::kTile + threadIdx.x;
-        Key key{a.pages, 0u};
-        if (threadIdx.x < (unsigned)S::kTile && unit < unit1 && j < length) {
-          const unsigned w = (unsigned)((unsigned long long)j * a.page_factor >> a.page_shift);
-          key.page = (unsigned)table[w];
-          key.place = j - w * a.page;
-        }
-        const unsigned long long mask = __ballot(key.page < a.pages);
-        if (threadIdx.x < (unsigned)S::kTile) keys[unit & 3][threadIdx.x] = key;
-        if (lane_id() == 0) there[unit & 3][wave] = mask;
-      }
+    // where the keys of a unit lie, a thread for each: its page is asked for a unit before it is written down
+    const bool looks = threadIdx.x < (unsigned)((S::kTile + kWave - 1) / kWave * kWave);
+    auto page_of = [&](unsigned unit) {
+      const unsigned j = unit * S::kTile + threadIdx.x;
+      const bool mine = threadIdx.x < (unsigned)S::kTile && unit < unit1 && j < length;
+      return mine ? (unsigned)table[(unsigned)((unsigned long long)j * a.page_factor >> a.page_shift)] : a.pages;
+    };
+    auto write_down = [&](unsigned unit, unsigned page) {
+      const unsigned j = unit * S::kTile + threadIdx.x, w = (unsigned)((unsigned long long)j * a.page_factor >> a.page_shift);
+      const unsigned long long mask = __ballot(page < a.pages);
+      // a key that is not there is read where the first page's first lies
+      if (threadIdx.x < (unsigned)S::kTile) keys[unit & 3][threadIdx.x] = page < a.pages ? Key{page * a.k_page + (j - w * a.page) * a.k_place, page * a.v_page + (j - w * a.page) * a.v_place} : Key{0, 0};
+      if (lane_id() == 0) there[unit & 3][wave] = mask;
     };
     Frag next_k[S::kLoads], next_v[S::kLoads];
-    const unsigned chunk = threadIdx.x % kRow, key0 = threadIdx.x / kRow;
     auto load = [&](unsigned unit) {
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         const Key key = keys[unit & 3][key0 + i * (kThreads / kRow)];
-        const bool mine = key.page < a.pages && chunk * kWide < a.dim;
-        Frag x, y;
-#pragma unroll
-        for (int e = 0; e < kWide; ++e) x[e] = y[e] = (T)0.0f;
-        if (mine) {
-          x = load_vec<T, kWide>(k0 + key.page * a.k_page + key.place * a.k_place + chunk * kWide);
-          y = load_vec<T, kWide>(v0 + key.page * a.v_page + key.place * a.v_place + chunk * kWide);
-        }
-        next_k[i] = x;
-        next_v[i] = y;
+        next_k[i] = load_vec<T, kWide>(k0 + key.k);
+        next_v[i] = load_vec<T, kWide>(v0 + key.v);
       }
     };
+    // whether all keys of a unit are there
+    auto is_whole = [&](unsigned unit) {
+      return there[unit & 3][0] == (S::kTile >= 64 ? ~0ull : (1ull << S::kTile % 64) - 1) && (S::kTile <= 64 || there[unit & 3][1] == ~0ull);
+    };
     __syncthreads();                                         // the row before is done with LDS
-    look_up(unit0);
-    look_up(unit0 + 1);
+    unsigned page = a.pages;
+    if (looks) {
+      const unsigned first = page_of(unit0), second = page_of(unit0 + 1);
+      page = page_of(unit0 + 2);
+      write_down(unit0, first);
+      write_down(unit0 + 1, second);
+    }
     __syncthreads();
     load(unit0);
     for (unsigned unit = unit0; unit < unit1; ++unit) {
       __syncthreads();                                       // the unit before is read
+      if (a.dim < (unsigned)Dim && chunk * kWide >= a.dim)   // past the end of a head, whose query is zero there
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i)
+#pragma unroll
+          for (int e = 0; e < kWide; ++e) next_k[i][e] = (T)0.0f;
+      if (!is_whole(unit))                                   // the weight of a key that is not there is zero, its value must not be more
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i) {
+          const unsigned key = key0 + i * (kThreads / kRow);
+          const bool mine = there[unit & 3][key / 64] >> key % 64 & 1;
+#pragma unroll
+          for (int e = 0; e < kWide; ++e) next_v[i][e] = mine ? next_v[i][e] : (T)0.0f;
+        }
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         const unsigned key = key0 + i * (kThreads / kRow);
         lds_k[place_in_lds<kRow>(key, chunk)] = next_k[i];
         lds_v[key * kRow + chunk] = next_v[i];
       }
-      look_up(unit + 2);
+      if (looks) write_down(unit + 2, page);
       __syncthreads();
-      load(unit + 1);
+      load(unit + 1 < unit1 ? unit + 1 : unit);
+      if (looks) page = page_of(unit + 3);
 #pragma unroll
       for (int step = 0; step < S::kSteps; ++step) {
         const unsigned first = (key_wave * S::kSteps + step) * kKeys;
@@ -252,9 +276,9 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
             Acc score = part[t][0];
-            if constexpr (kSums == 4) score = (part[t][0] + part[t][1]) + (part[t][2] + part[t][3]);
+            if constexpr (kSums == 4) score = ((part[t][0] + part[t][1]) + (part[t][2] + part[t][3])) * a.scale;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[t][u][i] = score[i] * a.scale;
+            for (int i = 0; i < 4; ++i) p[t][u][i] = score[i];
           }
         }
         if (live != (kKeys == 32 ? 0xffffffffu : 0xffffu)) {
@@ -273,20 +297,22 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
           for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, p[t][u][i]);
-          most = fmaxf(column_max(most), m[t]);
+          // 16 bits: m in powers of 2, one multiplication that is not rounded from a product to the exponent of its weight
+          most = fmaxf(column_max(most) * by, m[t]);
           const float top = most == -__builtin_inff() ? 0.0f : most;
           if (__any(most > m[t])) {
-            const float keep = exp_of(m[t] - top);
+            const float keep = power(m[t] - top);
             m[t] = most;
             l[t] *= keep;
 #pragma unroll
             for (int j = 0; j < kW; ++j) o[t][j] *= keep;
           }
+          const float off = (float)Kind<T>::kShift - top;
 #pragma unroll
           for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              p[t][u][i] = exp_of(p[t][u][i] - top, (float)Kind<T>::kShift);
+              p[t][u][i] = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(fmaf(p[t][u][i], by, off)) : exp_of(p[t][u][i] - top);
               l[t] += p[t][u][i];
             }
         }
@@ -354,7 +380,7 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
             const float other = *slot(w, 2 * t), most = fmaxf(m[t], other), base = most == -__builtin_inff() ? 0.0f : most;
-            const float keep = exp_of(m[t] - base), f = exp_of(other - base);
+            const float keep = power(m[t] - base), f = power(other - base);
             m[t] = most;
             l[t] = l[t] * keep + *slot(w, 2 * t + 1) * f;
 #pragma unroll
@@ -363,25 +389,31 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (ColumnWaves == 1 && Dim ==
               for (int i = 0; i < 4; ++i) o[t][j][i] = o[t][j][i] * keep + *slot(w, 4 + (t * kW + j) * 4 + i) * f;
           }
     }
+    // A lane's sums lie 16 bytes here and there in a piece; they pass through LDS, a tile of 16 columns at a time, so that a wave writes rows.
+    __syncthreads();                                         // all are done with LDS
     if (key_wave == 0) {
-      float *const piece = a.pieces + (size_t)(blockIdx.x + plan.rows[g] + row) * prefix_piece_floats(S::kColumns, a.dim);
+      const size_t floats = prefix_piece_floats(S::kColumns, a.dim);
+      float *const piece = a.pieces + (size_t)(blockIdx.x + plan.rows[g] + row) * floats, *const rows = reinterpret_cast<float *>(bytes) + wave * 16 * (Dim + 4);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
-        const unsigned column = column_wave * 16 * kTiles + 16 * t + r;
+        const unsigned first = column_wave * 16 * kTiles + 16 * t, live = min(columns - min(columns, column0 + 16 * t), 16u);
         const float sum = column_sum(l[t]);
-        if (column0 + 16 * t + r >= columns) continue;
+        if (live == 0) continue;
 #pragma unroll
         for (int n = 0; n < kParts; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const unsigned d = (n * 16 + 4 * g4 + i) * kPart;
-            if (d >= a.dim) continue;
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < kPart; e += 4)
-              store_vec<float, 4>(piece + (size_t)column * a.dim + d + e,
-                                  Vec<float, 4>{o[t][n * kPart + e][i], o[t][n * kPart + e + 1][i], o[t][n * kPart + e + 2][i], o[t][n * kPart + e + 3][i]});
-          }
-        if (g4 == 0) store_vec<float, 2>(piece + (size_t)S::kColumns * a.dim + 2 * column, Vec<float, 2>{m[t], sum});
+              *reinterpret_cast<Vec<float, 4> *>(rows + r * (Dim + 4) + (n * 16 + 4 * g4 + i) * kPart + e) =
+                  Vec<float, 4>{o[t][n * kPart + e][i], o[t][n * kPart + e + 1][i], o[t][n * kPart + e + 2][i], o[t][n * kPart + e + 3][i]};
+        __builtin_amdgcn_wave_barrier();
+        for (unsigned x = lane_id(); x < live * (Dim / 4); x += kWave) {
+          const unsigned column = x / (Dim / 4), d = x % (Dim / 4) * 4;
+          if (d < a.dim) store_vec<float, 4>(piece + (size_t)(first + column) * a.dim + d, *reinterpret_cast<const Vec<float, 4> *>(rows + column * (Dim + 4) + d));
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (g4 == 0 && r < live) store_vec<float, 2>(piece + (size_t)S::kColumns * a.dim + 2 * (first + r), Vec<float, 2>{sizeof(T) == 4 ? m[t] : m[t] * kLn2, sum});
       }
     }
     at += unit1 - unit0;
@@ -457,6 +489,8 @@ int make_prefix_attention(const fc_prefix_attention &n, std::unique_ptr<Operator
   op->any_prefix = groups > 0 && keys > 0 && n.k_cache.rank == 4 && n.k_cache.shape[0] > 0;
   op->own.form = op->any_prefix ? Form::kAfterPrefix : Form::kPlain;
   if (const int rc = settle_attention(own, op->own, err); rc != FC_OK) return rc;
+  // whose logarithm's base could not be changed in 32 bits
+  if (std::fabs(n.scale) >= 0x1p126) return c.fail(FC_E_UNSUPPORTED, "scale must be below 2^126").code();
   const AttentionArgs &o = op->own.a;
   if (op->any_prefix && o.requests && o.group) {
     PrefixArgs &a = op->a;

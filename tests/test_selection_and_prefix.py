@@ -117,6 +117,8 @@ REFUSED = [
     ("FC_E_ARG", lambda: prefix(out=T("bfloat16", 3, 4, 64, stride=(0, 64, 1)))),
     ("FC_E_ARG", lambda: prefix(lse=T("bfloat16", 3, 4))),
     ("FC_E_ARG", lambda: prefix(scale=math.nan)),
+    ("FC_E_ARG", lambda: prefix(scale=1e39)),
+    ("FC_E_UNSUPPORTED", lambda: prefix(scale=-1e38)),
     ("FC_E_ARG", lambda: prefix(k_cache=T("bfloat16", 9, 0, 2, 64), v_cache=T("bfloat16", 9, 0, 2, 64))),
     ("FC_E_UNSUPPORTED", lambda: prefix(dim=264)),
     ("FC_E_UNSUPPORTED", lambda: prefix(dim=60)),
