@@ -209,8 +209,9 @@ template <Form F, class T> __device__ __forceinline__ Share share_of(const Atten
   s.by_wave = F != Form::kAfterPrefix && uniform(any_long) == 0 && a.requests * rows > a.workers;
   // long rows keep a compute unit's memory pipe full with few workgroups, and the fewer they are the less is joined; short ones leave
   // gaps that others fill: one workgroup a compute unit and all that are resident take for a request of 131072 keys 88 and 102 us, 100 of 1000
-  // keys 75 and 84, 200 of up to 1000 89 and 84.5, 200 of up to 500 60 and 51
-  const unsigned workers = total >= kLongRow * a.requests * rows ? a.streams : a.workers;
+  // keys 75 and 84, 200 of up to 1000 89 and 84.5, 200 of up to 500 60 and 51.  Behind a prefix each row ends with the prefix' pieces, which others'
+  // keys hide: 200 requests of 1024 keys on average, 4 key heads 128 us and 115
+  const unsigned workers = F != Form::kAfterPrefix && total >= kLongRow * a.requests * rows ? a.streams : a.workers;
   s.share = max((total + workers - 1) / workers, 1u);
   s.at = (unsigned)min((unsigned long long)worker * s.share, (unsigned long long)total);
   s.end = min(s.at + s.share, total);

@@ -92,13 +92,22 @@ struct Key {
   long long k, v;
 };
 
+// 4 elements of 16 bits in LDS, which 16 lanes change among themselves: lane r gets the r-th of the 16 elements of lanes 0 to 3, of 4 to 7, of 8 to 11
+// and of 12 to 15
+template <class T> __device__ __forceinline__ Vec<T, 4> read_turned(const T *from) {
+  using Raw = Vec<short, 4>;
+  return __builtin_bit_cast(Vec<T, 4>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Raw *)reinterpret_cast<uintptr_t>(from)));
+}
+
 template <class T, int Dim, int ColumnWaves> struct PrefixShape {
   static constexpr int kTiles = sizeof(T) == 4 && Dim == 256 ? 1 : 2;        // of 16 columns of a wave, as many as its registers hold
   static constexpr int kColumns = 16 * kTiles * ColumnWaves, kKeyWaves = kWaves / ColumnWaves;
   static constexpr int kSteps = kKeyWaves == 1 ? 2 : 1, kTile = Kind<T>::kKeys * kKeyWaves * kSteps;
   static constexpr int kWide = 16 / sizeof(T), kRow = Dim / kWide;           // 16 bytes of a key; of them in a row
   static constexpr int kLoads = kTile * kRow / kThreads;                     // of K, and of V, of a thread
-  static constexpr size_t kTileBytes = 2 * (size_t)kTile * Dim * sizeof(T);
+  // 16 bits: 32 bytes between the values of two keys, so that the four rows that a turned read takes start at different banks
+  static constexpr int kValueRow = Dim + (sizeof(T) == 2 ? 16 : 0);
+  static constexpr size_t kTileBytes = (size_t)kTile * (Dim + kValueRow) * sizeof(T);
   static constexpr size_t kJoinBytes = (size_t)(kWaves - ColumnWaves) * (kTiles * Dim / 4 + 4) * kWave * sizeof(float);
   static constexpr size_t kRowsBytes = (size_t)ColumnWaves * 16 * (Dim + 4) * sizeof(float);
   static constexpr size_t kBytes = std::max({kTileBytes, kJoinBytes, kRowsBytes});
@@ -116,6 +125,8 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
   constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = S::kWide, kChunks = Dim / (4 * kWide), kRow = S::kRow;
   constexpr int kW = Dim / 16, kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;
   constexpr int kTiles = S::kTiles;
+  // weights of f16, 2^14 larger than they are, end at 2^16
+  constexpr float kSlack = sizeof(T) == 4 ? 5.0f : Kind<T>::kShift ? 1.0f : 8.0f;
   using Frag = Vec<T, kWide>;
   using Part = Vec<T, kPart>;
   __shared__ Plan plan;
@@ -124,25 +135,24 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
   __shared__ unsigned long long there[4][2];
   make_plan<S::kColumns, S::kTile>(a, plan);
   const unsigned total = plan.units[a.groups], share = max((total + a.workers - 1) / a.workers, 1u);
-  if (blockIdx.x == a.workers) {           // the last writes down what the others do, for the launch that joins it
-    if (threadIdx.x == 0) a.plan[0] = share;
-    for (unsigned b = threadIdx.x; b < a.requests; b += kThreads) {
-      unsigned words[8] = {};
-      if (b >= plan.starts[0] && b < plan.starts[a.groups]) {
-        const unsigned g = last_at_or_below(plan.starts, a.groups, b), n = plan.starts[g + 1] - plan.starts[g];
-        const unsigned rows = plan.rows[g + 1] - plan.rows[g];
-        words[0] = plan.units[g];
-        words[1] = rows ? (plan.units[g + 1] - plan.units[g]) / rows : 0u;
-        words[2] = b - plan.starts[g];
-        words[3] = ceil_div((unsigned long long)n * a.group, S::kColumns);
-        words[4] = plan.rows[g];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) a.plan[8 + 8 * (size_t)b + i] = words[i];
+  // what the others do is written down for the launch that joins it, some requests by each
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = share;
+  for (unsigned b = blockIdx.x * kThreads + threadIdx.x; b < a.requests; b += a.workers * kThreads) {
+    unsigned words[5] = {};
+    if (b >= plan.starts[0] && b < plan.starts[a.groups]) {
+      const unsigned g = last_at_or_below(plan.starts, a.groups, b), n = plan.starts[g + 1] - plan.starts[g];
+      const unsigned rows = plan.rows[g + 1] - plan.rows[g];
+      words[0] = plan.units[g];
+      words[1] = rows ? (plan.units[g + 1] - plan.units[g]) / rows : 0u;
+      words[2] = b - plan.starts[g];
+      words[3] = ceil_div((unsigned long long)n * a.group, S::kColumns);
+      words[4] = plan.rows[g];
     }
-    return;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) a.plan[8 + 8 * (size_t)b + i] = words[i];
   }
-  Frag *const lds_k = reinterpret_cast<Frag *>(bytes), *const lds_v = lds_k + S::kTile * kRow;
+  Frag *const lds_k = reinterpret_cast<Frag *>(bytes);
+  T *const lds_v = reinterpret_cast<T *>(bytes) + S::kTile * Dim;
   const unsigned r = lane_id() & 15, g4 = lane_id() >> 4;
   const unsigned wave = uniform((unsigned)wave_id()), column_wave = wave % ColumnWaves, key_wave = wave / ColumnWaves;
   const T *const q0 = reinterpret_cast<const T *>(a.q);
@@ -248,13 +258,13 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
       for (int i = 0; i < S::kLoads; ++i) {
         const unsigned key = key0 + i * (kThreads / kRow);
         lds_k[place_in_lds<kRow>(key, chunk)] = next_k[i];
-        lds_v[key * kRow + chunk] = next_v[i];
+        store_vec<T, kWide>(lds_v + key * S::kValueRow + chunk * kWide, next_v[i]);
       }
       if (looks) write_down(unit + 2, page);
       __syncthreads();
       load(unit + 1 < unit1 ? unit + 1 : unit);
       if (looks) page = page_of(unit + 3);
-#pragma unroll
+#pragma clang loop unroll_count(Dim == 256 ? 1 : S::kSteps)
       for (int step = 0; step < S::kSteps; ++step) {
         const unsigned first = (key_wave * S::kSteps + step) * kKeys;
         const unsigned live = (unsigned)(there[unit & 3][first / 64] >> first % 64) & (kKeys == 32 ? 0xffffffffu : 0xffffu);
@@ -272,6 +282,7 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
             const Frag k = lds_k[place_in_lds<kRow>(first + 16 * u + r, c * 4 + g4)];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) part[t][c % kSums] = mma(k, q[t][c], part[t][c % kSums]);
+            if (Dim == 256 && c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
           }
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
@@ -297,16 +308,18 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
           for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, p[t][u][i]);
-          // 16 bits: m in powers of 2, one multiplication that is not rounded from a product to the exponent of its weight
-          most = fmaxf(column_max(most) * by, m[t]);
-          const float top = most == -__builtin_inff() ? 0.0f : most;
-          if (__any(most > m[t])) {
-            const float keep = power(m[t] - top);
+          // m may stay behind the largest score by kSlack, so that sums are seldom multiplied.  16 bits: m in powers of 2, and one multiplication
+          // that is not rounded takes a product to the exponent of its weight.
+          most *= by;
+          if (__any(most > m[t] + kSlack)) {
+            most = fmaxf(column_max(most), m[t]);
+            const float keep = most == -__builtin_inff() ? 1.0f : power(m[t] - most);
             m[t] = most;
             l[t] *= keep;
 #pragma unroll
             for (int j = 0; j < kW; ++j) o[t][j] *= keep;
           }
+          const float top = m[t] == -__builtin_inff() ? 0.0f : m[t];
           const float off = (float)Kind<T>::kShift - top;
 #pragma unroll
           for (int u = 0; u < kSub; ++u)
@@ -316,14 +329,6 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
               l[t] += p[t][u][i];
             }
         }
-        Part vf[kSub][4][kParts];
-#pragma unroll
-        for (int u = 0; u < kSub; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < kParts; ++n)
-              vf[u][i][n] = *reinterpret_cast<const Part *>(reinterpret_cast<const T *>(lds_v + (first + 16 * u + 4 * g4 + i) * kRow) + (16 * n + r) * kPart);
         if constexpr (sizeof(T) == 2) {
           Vec<T, 8> high[kTiles], low[kTiles];
 #pragma unroll
@@ -335,24 +340,29 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
               high[t][e] = upper;
               low[t][e] = rest;
             }
+          // a read gives each lane r the element 16 j + r of the keys 4g .. 4g+3: it takes four elements of key 4g + r / 4 and has them change lanes
+          const T *const from = lds_v + (first + 4 * g4 + r / 4) * S::kValueRow + r % 4 * 4;
 #pragma unroll
-          for (int n = 0; n < kParts; ++n)
+          for (int j = 0; j < kW; ++j) {
+            const Vec<T, 8> values = __builtin_shufflevector(read_turned(from + 16 * j), read_turned(from + 16 * S::kValueRow + 16 * j), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int e = 0; e < kPart; ++e) {
-              const Vec<T, 8> values = {vf[0][0][n][e], vf[0][1][n][e], vf[0][2][n][e], vf[0][3][n][e], vf[1][0][n][e], vf[1][1][n][e], vf[1][2][n][e], vf[1][3][n][e]};
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t) {
-                Acc &sums = o[t][n * kPart + e];
-                sums = mma(values, high[t], sums);
-                sums = mma(values, low[t], sums);
-              }
+            for (int t = 0; t < kTiles; ++t) {
+              o[t][j] = mma(values, high[t], o[t][j]);
+              o[t][j] = mma(values, low[t], o[t][j]);
             }
+            if (Dim == 256 && j % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // no further reads ahead: registers
+          }
         } else {
+          Part vf[4][kParts];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) vf[i][n] = load_vec<T, kPart>(lds_v + (first + 4 * g4 + i) * S::kValueRow + (16 * n + r) * kPart);
 #pragma unroll
           for (int j = 0; j < kW; ++j)
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
-              o[t][j] = mma(Vec<float, 4>{vf[0][0][j / kPart][j % kPart], vf[0][1][j / kPart][j % kPart], vf[0][2][j / kPart][j % kPart], vf[0][3][j / kPart][j % kPart]},
+              o[t][j] = mma(Vec<float, 4>{vf[0][j / kPart][j % kPart], vf[1][j / kPart][j % kPart], vf[2][j / kPart][j % kPart], vf[3][j / kPart][j % kPart]},
                             Vec<float, 4>{p[t][0][0], p[t][0][1], p[t][0][2], p[t][0][3]}, o[t][j]);
         }
       }
@@ -399,14 +409,17 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
         const unsigned first = column_wave * 16 * kTiles + 16 * t, live = min(columns - min(columns, column0 + 16 * t), 16u);
         const float sum = column_sum(l[t]);
         if (live == 0) continue;
+        float *const mine = rows + r * (Dim + 4);
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int n = 0; n < kParts; ++n)
+          for (int j = 0; j < kW; ++j) store_vec<float, 4>(mine + 16 * j + 4 * g4, o[t][j]);
+        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int n = 0; n < kParts; ++n)
 #pragma unroll
-            for (int e = 0; e < kPart; e += 4)
-              *reinterpret_cast<Vec<float, 4> *>(rows + r * (Dim + 4) + (n * 16 + 4 * g4 + i) * kPart + e) =
-                  Vec<float, 4>{o[t][n * kPart + e][i], o[t][n * kPart + e + 1][i], o[t][n * kPart + e + 2][i], o[t][n * kPart + e + 3][i]};
+            for (int i = 0; i < 4; ++i)
+              store_vec<float, 4>(mine + (n * 16 + 4 * g4 + i) * kPart, Vec<float, 4>{o[t][n * kPart][i], o[t][n * kPart + 1][i], o[t][n * kPart + 2][i], o[t][n * kPart + 3][i]});
+        }
         __builtin_amdgcn_wave_barrier();
         for (unsigned x = lane_id(); x < live * (Dim / 4); x += kWave) {
           const unsigned column = x / (Dim / 4), d = x % (Dim / 4) * 4;
@@ -429,9 +442,13 @@ template <class T, int Dim, int ColumnWaves> Variant variant() {
   using S = PrefixShape<T, Dim, ColumnWaves>;
   return {&prefix_kernel<T, Dim, ColumnWaves>, (unsigned)S::kColumns, (unsigned)S::kTile};
 }
+// the largest heads leave no registers for waves of other keys
 template <class T, int Dim> Variant variant_of_heads(unsigned columns) {
-  if constexpr (Dim == 256) return columns <= 2 * 16 * PrefixShape<T, Dim, 2>::kTiles ? variant<T, Dim, 2>() : variant<T, Dim, 4>();
-  else return columns <= 32 ? variant<T, Dim, 1>() : columns <= 64 ? variant<T, Dim, 2>() : variant<T, Dim, 4>();
+  if constexpr (Dim < 256)
+    if (columns <= 32) return variant<T, Dim, 1>();
+  if constexpr (Dim < 256 || sizeof(T) == 4)
+    if (columns <= 32 * PrefixShape<T, Dim, 2>::kTiles) return variant<T, Dim, 2>();
+  return variant<T, Dim, 4>();
 }
 template <class T> Variant variant_of_type(unsigned dim, unsigned columns) {
   return dim <= 64 ? variant_of_heads<T, 64>(columns) : dim <= 128 ? variant_of_heads<T, 128>(columns) : variant_of_heads<T, 256>(columns);
@@ -454,7 +471,7 @@ struct PrefixAttention final : Operator {
     PrefixArgs args = a;
     args.plan = reinterpret_cast<unsigned *>(r.workspace);
     args.pieces = reinterpret_cast<float *>(r.workspace + plan_bytes());
-    r.launch(variant.kernel, a.workers + 1, kThreads, args);
+    r.launch(variant.kernel, a.workers, kThreads, args);
     Recorder behind{r.launches, r.workspace + plan_bytes() + pieces_bytes(), r.counters, r.what};
     Attention after = own;
     after.a.prefix_plan = args.plan;
