@@ -74,7 +74,7 @@ struct Attention : Operator {
   void record(Recorder &r) const override;
   const char *name() const override { return "paged attention"; }
 };
-// The arrays that all forms have, checked and entered into `op`, whose form is set; `requests` and `kv` come back.
+// The arrays that all forms have, checked and entered into `op`, whose form is set.
 int settle_attention(const fc_paged_attention &n, Attention &op, std::string &err);
 
 namespace {

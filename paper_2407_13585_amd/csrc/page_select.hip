@@ -29,7 +29,8 @@ struct SelectArgs {
   unsigned long long *keys;                // DEVICE: of each row `width`; NULL: they fit LDS
   unsigned *counters;                      // DEVICE: one a row, 0 between launches
   long long q_request, q_head, b_page, b_head, b_half, table_stride, s_request, s_head, l_request;
-  unsigned requests, heads, group, dim, page, pages, width, most, first, last, parts;
+  unsigned requests, heads, group, dim, page, pages, width, most, first, last;
+  unsigned pieces;                         // of about the same size that all rows together are split into, and one more a row; 0: they are not
 };
 
 // a number that orders scores as they are; NaN counts as infinite, -0 as 0
@@ -172,15 +173,14 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, unsigned all) 
   return before == all - 1;
 }
 
-// The sums of two numbers over the workgroup up to this thread, and in all.
+// The sums of two numbers that a wave's lanes share, over the waves before this one and in all.
 struct Sums {
   unsigned x, y, all_x, all_y;
 };
-__device__ __forceinline__ Sums sum_up_to(unsigned x, unsigned y, unsigned (*lds)[2]) {
-  const unsigned to_x = (unsigned)wave_scan_inclusive<AddI32>((int)x), to_y = (unsigned)wave_scan_inclusive<AddI32>((int)y);
-  if (lane_id() == kWave - 1) { lds[wave_id()][0] = to_x; lds[wave_id()][1] = to_y; }
+__device__ __forceinline__ Sums sum_of_waves(unsigned x, unsigned y, unsigned (*lds)[2]) {
+  if (lane_id() == 0) { lds[wave_id()][0] = x; lds[wave_id()][1] = y; }
   __syncthreads();
-  Sums s{to_x, to_y, 0, 0};
+  Sums s{0, 0, 0, 0};
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave_id()) { s.x += lds[w][0]; s.y += lds[w][1]; }
@@ -189,85 +189,91 @@ __device__ __forceinline__ Sums sum_up_to(unsigned x, unsigned y, unsigned (*lds
   }
   return s;
 }
+__device__ __forceinline__ unsigned lanes_of(bool b) { return (unsigned)__popcll(__ballot(b)); }
+// the lanes of `mask` before this one
+__device__ __forceinline__ unsigned lanes_before(unsigned long long mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u)); }
 
-// keys of a row in memory
-__device__ __host__ __forceinline__ size_t far_keys(unsigned width) { return ((size_t)width + kThreads - 1) / kThreads * kThreads; }
+__device__ __forceinline__ unsigned length_of(const SelectArgs &a, int length) { return (unsigned)min((unsigned long long)max(length, 0), (unsigned long long)a.width * a.page); }
+__device__ __forceinline__ unsigned pages_of(const SelectArgs &a, unsigned length) { return (length + a.page - 1) / a.page; }
+// no more pages than are wanted: all that are there are taken
+__device__ __forceinline__ bool is_scored(const SelectArgs &a, unsigned count) { return count > a.most && a.pages > 0; }
+// of a row: kBlockPages pages that are scored, or one
+__device__ __forceinline__ unsigned units_of(const SelectArgs &a, unsigned count) { return is_scored(a, count) ? (count + kBlockPages - 1) / kBlockPages : 1u; }
 
+// Scores the units [unit0, unit1) of the row of request b and key head `head`; the last of the `parts` workgroups that it is split over, who count on
+// `counter`, then selects.
 // Held: keys of a row that a thread keeps in registers, side by side; 0: as many as there are, read again whenever they are looked at
-template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+template <class T, int HeadTiles, bool Whole, int Held>
+__device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, unsigned head, unsigned length, unsigned unit0, unsigned unit1, unsigned parts, unsigned *counter) {
   __shared__ unsigned long long kept[kKept];
   __shared__ unsigned counts[2][256], sums[2][kWaves][2], found[2][3];
   __shared__ int ends[2][kWaves];
   __shared__ unsigned listed[kListed];
-  const unsigned row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-  const unsigned b = row / a.heads, head = row - b * a.heads;
-  const unsigned length = (unsigned)min((unsigned long long)max(load_scalar(a.lengths + b), 0), (unsigned long long)a.width * a.page);
-  const unsigned count = (length + a.page - 1) / a.page;
+  const unsigned count = pages_of(a, length);
   const int *const table = a.table + b * a.table_stride;
   int *const selected = a.selected + b * a.s_request + head * a.s_head;
-  unsigned long long *const far = a.keys ? a.keys + (size_t)row * far_keys(a.width) : nullptr;
-  const bool scored = count > a.most && a.pages > 0;                        // else all that are there are taken
-  const unsigned parts = scored ? min(a.parts, (count + kBlockPages - 1) / kBlockPages) : 1u;
-  if (part >= parts) return;
+  unsigned long long *const far = a.keys ? a.keys + (size_t)(b * a.heads + head) * a.width : nullptr;
+  const bool scored = is_scored(a, count);
   const bool near = parts == 1 && count <= kKept;            // the keys never leave LDS
-  // each thread has positions of its own, side by side; in memory their keys lie so that a wave reads neighbours
-  const unsigned each = (count + kThreads - 1) / kThreads, w0 = min(threadIdx.x * each, count), w1 = min(w0 + each, count);
+  // a wave has `each` times 64 positions side by side, a lane one of every 64
+  const unsigned each = (count + kThreads - 1) / kThreads, w0 = (unsigned)wave_id() * each * kWave + lane_id();
   if (scored) {
     const T *const q = reinterpret_cast<const T *>(a.q) + b * a.q_request + head * a.group * a.q_head;
     const T *const bounds = reinterpret_cast<const T *>(a.bounds) + head * a.b_head;
     Scores<T, HeadTiles, Whole> scores(a, q, bounds, table);
-    for (unsigned at = part * kBlockPages; at < count; at += parts * kBlockPages)
+    for (unsigned at = unit0 * kBlockPages; at < min(unit1 * kBlockPages, count); at += kBlockPages)
       scores.run(at + kBlockPages / kWaves * (unsigned)wave_id(), min(at + kBlockPages, count), [&](unsigned w, bool there, double s, bool first) {
         unsigned long long key = !there ? 0ull : w < a.first || w + a.last >= count ? kAlways : key_of(s);
         if (near) kept[w] = first ? key : max(kept[w], key);
         else {
-          unsigned long long *const to = far + w / each + (size_t)(w % each) * kThreads;
+          unsigned long long *const to = far + w;
           store_agent64(to, first ? key : max(load_agent64(to), key));
         }
       });
   }
   if (parts > 1) {
-    if (!last_to_arrive(a.counters + row, parts)) return;
+    if (!last_to_arrive(counter, parts)) return;
   } else {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
-  // N keys from the thread's i0-th on, all read before the first is waited for; 0 behind its last
+  // N keys from the lane's i0-th on, all read before the first is waited for; 0 behind its last
   auto read_keys = [&](unsigned i0, auto &to) {
     constexpr int n = sizeof(to) / sizeof(to[0]);
     if (!scored) {
       unsigned page[n];
 #pragma unroll
       for (int i = 0; i < n; ++i)
-        if (i0 + i < each) page[i] = (unsigned)table[min(w0 + i0 + i, count - 1)];
+        if (i0 + i < each) page[i] = (unsigned)table[min(w0 + (i0 + i) * kWave, count - 1)];
 #pragma unroll
-      for (int i = 0; i < n; ++i) to[i] = w0 + i0 + i < w1 && page[i] < a.pages ? kAlways : 0ull;
+      for (int i = 0; i < n; ++i) to[i] = i0 + i < each && w0 + (i0 + i) * kWave < count && page[i] < a.pages ? kAlways : 0ull;
     } else {
       if (near)
 #pragma unroll
-        for (int i = 0; i < n; ++i) to[i] = kept[min(w0 + i0 + i, count - 1)];
+        for (int i = 0; i < n; ++i) to[i] = kept[min(w0 + (i0 + i) * kWave, count - 1)];
       else
 #pragma unroll
         for (int i = 0; i < n; ++i)
-          if (i0 + i < each) to[i] = load_agent64(far + threadIdx.x + (size_t)(i0 + i) * kThreads);
+          if (i0 + i < each) to[i] = load_agent64(far + min(w0 + (i0 + i) * kWave, count - 1));
 #pragma unroll
-      for (int i = 0; i < n; ++i) to[i] = w0 + i0 + i < w1 ? to[i] : 0ull;
+      for (int i = 0; i < n; ++i) to[i] = i0 + i < each && w0 + (i0 + i) * kWave < count ? to[i] : 0ull;
     }
   };
   unsigned long long held[Held ? Held : 1];
   if constexpr (Held > 0) read_keys(0, held);
+  // use(position, key) by all lanes together
   auto for_keys = [&](auto &&use) {
     if constexpr (Held > 0) {
 #pragma unroll
       for (int i = 0; i < Held; ++i)
-        if (held[i] != 0) use(w0 + i, held[i]);
+        if ((unsigned)i < each) use(w0 + i * kWave, held[i]);
     } else {
       for (unsigned i0 = 0; i0 < each; i0 += 8) {
         unsigned long long some[8];
         read_keys(i0, some);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (some[i] != 0) use(w0 + i0 + i, some[i]);
+          if (i0 + i < each) use(w0 + (i0 + i) * kWave, some[i]);
       }
     }
   };
@@ -281,9 +287,9 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
     int least = INT32_MIN, largest = INT32_MIN;
     unsigned mine = 0, always = 0;
     for_keys([&](unsigned, unsigned long long key) {
-      ++mine;
-      always += key == kAlways;
-      if (key != kAlways) {
+      mine += lanes_of(key != 0);
+      always += lanes_of(key == kAlways);
+      if (key != 0 && key != kAlways) {
         const int upper = (int)((unsigned)(key >> 32) ^ 0x80000000u);
         least = max(least, ~upper);
         largest = max(largest, upper);
@@ -293,7 +299,7 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
     largest = wave_reduce<MaxI32>(largest);
     if (lane_id() == 0) { ends[0][wave_id()] = least; ends[1][wave_id()] = largest; }
     counts[0][threadIdx.x] = 0;
-    const Sums there = sum_up_to(mine, always, sums[turn]);
+    const Sums there = sum_of_waves(mine, always, sums[turn]);
     turn ^= 1;
     all = there.all_x <= a.most;
     const unsigned wanted = a.most - min(there.all_y, a.most);                 // of those that are not taken anyway
@@ -308,7 +314,7 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
         const unsigned digit = min(shift, 8u), upper = shift;
         shift -= digit;
         for_keys([&](unsigned, unsigned long long key) {
-          if (key != kAlways && (upper == 64 ? 0 : key >> upper) == bar) atomicAdd(&counts[n][key >> shift & ((1u << digit) - 1)], 1u);
+          if (key != 0 && key != kAlways && (upper == 64 ? 0 : key >> upper) == bar) atomicAdd(&counts[n][key >> shift & ((1u << digit) - 1)], 1u);
         });
         __syncthreads();
         if (wave_id() == 0) {                                                  // from the largest digit down: the one where `level` is reached
@@ -336,27 +342,32 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
       }
     }
   }
+  // the bar's keys are those from `low` up to `high`
+  const unsigned long long low = bar << shift, high = low + ((1ull << shift) - 1);
   unsigned above = 0, at_bar = 0;
   for_keys([&](unsigned, unsigned long long key) {
-    const unsigned long long cut = key >> shift;
-    const bool over = all || key == kAlways || cut > bar;
-    above += over;
-    at_bar += !over && cut == bar;
+    const bool over = key > high || (all && key != 0) || key == kAlways;
+    above += lanes_of(over);
+    at_bar += lanes_of(!over && key != 0 && key >= low);
   });
-  const Sums to = sum_up_to(above, at_bar, sums[turn]);
-  unsigned at_before = to.y - at_bar, slot = to.x - above + min(at_before, level);
+  const Sums to = sum_of_waves(above, at_bar, sums[turn]);
+  unsigned at_before = to.y, slot0 = to.x + min(at_before, level);
   const unsigned taken = min(to.all_x + min(to.all_y, level), a.most);
   bool is_last = false;
   for_keys([&](unsigned w, unsigned long long key) {
-    const unsigned long long cut = key >> shift;
-    bool take = all || key == kAlways || cut > bar;
-    if (!take && cut == bar) take = at_before++ < level;
+    const bool over = key > high || (all && key != 0) || key == kAlways;
+    const bool at = !over && key != 0 && key >= low;
+    const unsigned long long equal = __ballot(at);
+    const bool take = over || (at && at_before + lanes_before(equal) < level);
+    const unsigned long long mask = __ballot(take);
+    const unsigned slot = slot0 + lanes_before(mask);
     if (take && slot < a.most) {
       if (slot < kListed) listed[slot] = w;
       else selected[slot] = table[w];
-      ++slot;
       is_last |= w + 1 == count;
     }
+    at_before += (unsigned)__popcll(equal);
+    slot0 += (unsigned)__popcll(mask);
   });
   const unsigned short_of = __syncthreads_or(is_last) ? count * a.page - length : 0u;
   for (unsigned k = threadIdx.x; k < min(taken, kListed); k += kThreads) selected[k] = table[listed[k]];
@@ -364,7 +375,60 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
   if (threadIdx.x == 0) a.selected_lengths[b * a.l_request + head] = (int)(taken * a.page - short_of);
 }
 
-// workgroups of a call: more rows than these have one each
+template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+  unsigned b, length, units, unit0 = 0, unit1, parts = 1, head;
+  if (a.pieces == 0) {
+    b = blockIdx.x / a.heads;
+    head = blockIdx.x - b * a.heads;
+    length = length_of(a, load_scalar(a.lengths + b));
+    unit1 = units_of(a, pages_of(a, length));
+  } else {
+    __shared__ unsigned ends[kThreads], sums[2][kWaves];     // pieces of the rows of a thread's requests, summed up to it
+    const unsigned each = (a.requests + kThreads - 1) / kThreads, b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
+    unsigned mine = 0;
+    for (unsigned i = b0; i < b1; ++i) mine += units_of(a, pages_of(a, length_of(a, a.lengths[i]))) * a.heads;
+    mine = (unsigned)wave_reduce<AddI32>((int)mine);
+    if (lane_id() == 0) sums[0][wave_id()] = mine;
+    __syncthreads();
+    unsigned total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += sums[0][w];
+    const unsigned share = max((total + a.pieces - 1) / a.pieces, 1u);
+    auto parts_of = [&](unsigned n) { return (n + share - 1) / share; };
+    mine = 0;
+    for (unsigned i = b0; i < b1; ++i) mine += parts_of(units_of(a, pages_of(a, length_of(a, a.lengths[i])))) * a.heads;
+    const unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)mine);
+    if (lane_id() == kWave - 1) sums[1][wave_id()] = upto;
+    __syncthreads();
+    unsigned before = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (w < wave_id()) before += sums[1][w];
+    ends[threadIdx.x] = before + upto;
+    __syncthreads();
+    if (blockIdx.x >= ends[kThreads - 1]) return;
+    // the request of this piece, and the pieces before it
+    unsigned chunk = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / kWave; ++k) chunk += (unsigned)__popcll(__ballot(ends[k * kWave + lane_id()] <= blockIdx.x));
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+    before = chunk ? __builtin_amdgcn_readfirstlane(ends[chunk - 1]) : 0u;
+    for (b = chunk * each;; ++b) {
+      length = length_of(a, load_scalar(a.lengths + b));
+      units = units_of(a, pages_of(a, length));
+      parts = parts_of(units);
+      if (blockIdx.x - before < parts * a.heads) break;
+      before += parts * a.heads;
+    }
+    head = (blockIdx.x - before) / parts;
+    const unsigned part = blockIdx.x - before - head * parts;
+    unit0 = (unsigned)((unsigned long long)units * part / parts);
+    unit1 = (unsigned)((unsigned long long)units * (part + 1) / parts);
+  }
+  select_of_row<T, HeadTiles, Whole, Held>(a, b, head, length, unit0, unit1, parts, a.counters + (parts > 1 ? b * a.heads + head : 0));
+}
+
+// with more rows than half of these, each has a workgroup
 constexpr unsigned kWorkgroups = 2048;
 
 struct PageSelect final : Operator {
@@ -393,13 +457,13 @@ struct PageSelect final : Operator {
     else if (dtype == FC_F16) by_group(_Float16{});
     else by_group(__bf16{});
   }
-  size_t workspace() const override { return far ? (size_t)a.requests * a.heads * far_keys(a.width) * sizeof(unsigned long long) : 0; }
+  size_t workspace() const override { return far ? (size_t)a.requests * a.heads * a.width * sizeof(unsigned long long) : 0; }
   void record(Recorder &r) const override {
     if (a.requests == 0 || a.heads == 0) return;
     SelectArgs args = a;
     args.keys = far ? reinterpret_cast<unsigned long long *>(r.workspace) : nullptr;
     args.counters = r.counters;
-    with_kernel([&](auto kernel) { r.launch(kernel, a.requests * a.heads * a.parts, kThreads, args); });
+    with_kernel([&](auto kernel) { r.launch(kernel, a.pieces + a.requests * a.heads, kThreads, args); });
   }
   const char *name() const override { return "page select"; }
 };
@@ -459,9 +523,15 @@ int make_page_select(const fc_page_select &n, std::unique_ptr<Operator> &out, st
   // no more than the pages of a request of 2^31-1 keys are looked at
   a.width = (unsigned)std::min<uint64_t>(width, (0x7fffffffu + (uint64_t)a.page - 1) / a.page);
   const unsigned rows = a.requests * a.heads;
-  a.parts = rows && rows <= (unsigned)kCounters ? std::max(1u, std::min(kWorkgroups / rows, ceil_div(a.width, kBlockPages))) : 1u;
-  op->far = a.width > kKept || a.parts > 1;
+  const unsigned units = std::max(1u, ceil_div(a.width, kBlockPages));
+  const bool split = rows <= kWorkgroups / 2 && units > 1;
+  op->far = a.width > kKept || split;
   if ((uint64_t)rows * a.width > (uint64_t)1 << 36) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
+  if (split) {
+    unsigned resident = 0;
+    op->with_kernel([&](auto kernel) { resident = resident_workgroups(kernel, kThreads); });
+    a.pieces = std::min(resident ? resident : 1024u, rows * units);
+  }
   out = std::move(op);
   return FC_OK;
 }

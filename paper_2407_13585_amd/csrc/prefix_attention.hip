@@ -35,7 +35,7 @@ struct Plan {
   unsigned starts[kPrefixGroups + 1], rows[kPrefixGroups + 1], units[kPrefixGroups + 1];
 };
 
-template <int Columns, int Tile> __device__ __forceinline__ unsigned keys_of_group(const PrefixArgs &a, unsigned g) {
+__device__ __forceinline__ unsigned keys_of_group(const PrefixArgs &a, unsigned g) {
   return a.pages ? (unsigned)min((unsigned long long)max(a.lengths[g], 0), (unsigned long long)a.width * a.page) : 0u;
 }
 
@@ -67,7 +67,7 @@ template <int Columns, int Tile> __device__ __forceinline__ void make_plan(const
       unsigned rows = 0, units = 0;
       if (g < a.groups) {
         const unsigned n = plan.starts[g + 1] - plan.starts[g];
-        units = n ? ceil_div(keys_of_group<Columns, Tile>(a, g), Tile) : 0u;
+        units = n ? ceil_div(keys_of_group(a, g), Tile) : 0u;
         rows = units ? a.kv_heads * ceil_div((unsigned long long)n * a.group, Columns) : 0u;
         units *= rows;
       }
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
   while (at < end) {
     const unsigned g = uniform(last_at_or_below(plan.units, a.groups, at));
     const unsigned members = plan.starts[g + 1] - plan.starts[g], blocks = ceil_div((unsigned long long)members * a.group, S::kColumns);
-    const unsigned length = uniform(keys_of_group<S::kColumns, S::kTile>(a, g)), units = ceil_div(length, S::kTile);
+    const unsigned length = uniform(keys_of_group(a, g)), units = ceil_div(length, S::kTile);
     const unsigned row = uniform((at - plan.units[g]) / units), unit0 = at - plan.units[g] - row * units, unit1 = min(units, unit0 + (end - at));
     const unsigned kv = row / blocks, column0 = (row - kv * blocks) * S::kColumns + column_wave * 16 * kTiles;
     const unsigned columns = members * a.group;
