@@ -24,6 +24,13 @@
 //   of 256 (bf16, 2147 MB) 313 us, 6.9 TB/s, of 192 253 us, 6.4 TB/s; 37 requests in windows of 1000 keys, 6 key heads of 96, pages of 24 (f32, 111 MB)
 //   28 to 30 us, 3.7 to 4.0 TB/s, where the six units of a workgroup are too few to hide its start and end; 4 requests of up to 300 keys,
 //   2 key heads of 64 (f16) 7.1 us.
+//
+// The forms beside that share the kernel's code and differ in where a row's table and length lie and in how it ends.  A table for each key head: the rows of lengths
+// are those of requests and key heads; 64 requests, 8 key heads, 64 pages of 32 keys each (bf16, 521 MB) 92 us, 5.7 TB/s; one request of 128 pages a head
+// 13 us, the chain of reads.  Behind a prefix: whoever has the whole of a row joins its prefix' pieces as well, eight at a time; 200 requests of 1024 keys on
+// average, 4 key heads of 128 behind a prefix of 4096 (bf16, 430 MB and 40 of pieces) 112 to 124 us, 4.2 TB/s; 64 of 500, 8 key heads behind 32768 keys
+// (131 MB and 38 of pieces) 50 to 60 us, rows of four units whose ends and joins little else covers.  That form takes no row by a wave, which
+// would leave the prefix' pieces to a wave each.
 #pragma once
 
 #include "operators.hpp"

@@ -2,7 +2,12 @@
 //
 // A minimum and a maximum need nothing but the keys that are new and what the page's bounds were before, so a step reads no key twice.  A wave
 // takes a page and key head at a time: 16 bytes a lane, the lanes of a key side by side, several keys in an instruction and four instructions under way;
-// the lanes that hold other keys of the same elements then compare theirs.
+// the lanes that hold other keys of the same elements then compare theirs.  Pages with new keys, times heads, of all requests are one row, of which every
+// wave has an equal share: a step appends a key to each request or a prompt to a few, and either is spread over the device.
+//
+// Reading the new keys once bounds it where they are many: 40 prompts, 65536 keys of 8 heads of 128 in pages of 32 (bf16, 143 MB) 29.7 us, 4.8 TB/s; the launch and a
+// chain of reads (lengths, page, keys and what was there) where they are not: 64 requests with a key each (bf16) and 37 prompts of 9999 keys,
+// 3 heads of 80 (f32, 10 MB), 5.6 us.
 #include "operators.hpp"
 
 #include <algorithm>

@@ -6,7 +6,13 @@
 //
 // The scores become whole numbers of 64 bits in the same order; the k-th largest is found from its upper digits down, 8 bits at a time, from
 // the first that differs between the least and the largest on, until the pages above and at it are as many as are wanted.  One workgroup does it
-// for a request and key head; where these are few and their pages many, other workgroups help with the scores, and the last to be done selects.
+// for a request and key head (a row); where rows are few and their pages many, a row's scores are split into pieces of about the same size, and the last
+// workgroup to be done selects.
+//
+// What bounds it.  One request of 4096 pages of 8 key heads of 128, 64 heads (bf16, 17 MB) 30 us: 5 to the row's workgroup and its table, 8 for the scores
+// (reads 4, arithmetic 4, each once and one behind the other), 3 to hand them to one workgroup, 13 of that workgroup alone for 16 keys a lane.  64 requests of up to 1024 pages, 8
+// key heads of 128, 32 heads (bf16, 134 MB) 56 us: without selection 48.5, without most of the arithmetic too 42.5, without the table's reads 35, so
+// 3.8 TB/s of what it must read; 300 requests of 900 pages (bf16, 1.1 GB) 250 us, 4.4 TB/s, in 32 bits 442 us, 5.0 TB/s.  4 short requests 3.8 us: the launch.
 #include "operators.hpp"
 
 #include <algorithm>
@@ -16,9 +22,10 @@ namespace fc {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kTilesOfWave = 1;                             // of 16 pages, that a wave reads before it scores them
+// of 16 pages, that a wave reads before it scores them: two take 67 us where one takes 61 (64 ragged requests), 15.4 and 12.5 (19 in f32)
+constexpr int kTilesOfWave = 1;
 constexpr unsigned kBlockPages = 16 * kTilesOfWave * kWaves; // of a row that a workgroup scores at a time
-constexpr unsigned kKept = 1024;                             // keys that stay in LDS where one workgroup has a whole row
+constexpr unsigned kKept = 1024;                             // keys that stay in LDS where one workgroup has a whole row (300 requests of 900 pages 245 us, 264 by memory)
 constexpr unsigned kListed = 2048;                           // selected positions that are put in order in LDS
 constexpr unsigned long long kAlways = ~0ull;                // above every score; 0, below every score, is a page that is not there
 
@@ -49,7 +56,9 @@ template <int Ctrl> __device__ __forceinline__ double of_four(double v) {
 
 // Scores of pages for the query heads of a key head.  The instruction has four products of 4 pages, 4 elements and 4 heads: lane (r, g), r = lane % 16,
 // g = lane / 16, holds elements of page r, and of query head r % 4 the same ones; lane (4 n + j, i) gets page 4 n + i and head j.
-// HeadTiles: four query heads each that are taken together.  Whole: the elements of a head fill the lanes' reads.
+// HeadTiles: four query heads each that are taken together; groups of more than four take two at a time (32 requests of 2000 pages, groups of 8: 106 us, 126
+// with one), others one, whose second would be empty (64 of 1024 pages, groups of 4: 70 us, 98 with two).
+// Whole: the elements of a head fill the lanes' reads (32 requests of 2000 pages 106 us, 142 with the tests that other heads need).
 template <class T, int HeadTiles, bool Whole> struct Scores {
   static constexpr int N = 16 / sizeof(T), kChunks = 4, kTiles = kTilesOfWave;  // 16 bytes of each of four lanes; of them, and of 16 pages, under way
   using Part = Vec<T, N>;
@@ -202,7 +211,8 @@ __device__ __forceinline__ unsigned units_of(const SelectArgs &a, unsigned count
 
 // Scores the units [unit0, unit1) of the row of request b and key head `head`; the last of the `parts` workgroups that it is split over, who count on
 // `counter`, then selects.
-// Held: keys of a row that a thread keeps in registers, side by side; 0: as many as there are, read again whenever they are looked at
+// Held: keys of a row that a lane keeps in registers, no more than a call's tables need; 0: as many as there are, read again whenever they are looked at
+// (one request of 8192 pages 50 us with its keys held and 65 without; 32 of 2000 pages 106, 112 without, 118 with registers for four times as many).
 template <class T, int HeadTiles, bool Whole, int Held>
 __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, unsigned head, unsigned length, unsigned unit0, unsigned unit1, unsigned parts, unsigned *counter) {
   __shared__ unsigned long long kept[kKept];
@@ -428,7 +438,8 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
   select_of_row<T, HeadTiles, Whole, Held>(a, b, head, length, unit0, unit1, parts, a.counters + (parts > 1 ? b * a.heads + head : 0));
 }
 
-// with more rows than half of these, each has a workgroup
+// With more rows than half of these, each has a workgroup.  Pieces: as many as workgroups are resident; half of them take 60 us where these take 56 (64 ragged
+// requests), twice as many 57, a fixed number of pieces for every row 61.
 constexpr unsigned kWorkgroups = 2048;
 
 struct PageSelect final : Operator {

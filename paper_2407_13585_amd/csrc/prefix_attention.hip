@@ -5,6 +5,15 @@
 //   scores  = K q^T, outputs = V^T p^T, as in attention.hpp: lane (r, g), r = lane % 16, g = lane / 16, has columns r and 16 + r and the
 //   keys 4g .. 4g+3 of every 16, in whose order the values' product takes them from LDS.
 // What a workgroup has of a row (prefix.hpp) is written as it is: the attention of the requests' own keys, which follows, joins it.
+//
+// A step of 32 keys (16 of 32 bits) costs a wave 2 * 4 products for the scores and 3 * 8 for the values (128 elements of 16 bits), about 6 vector
+// instructions for each of its 16 scores a lane, and 16 kB from LDS; the three add up, since all waves of a workgroup come to each of them at about the same time.
+// A unit's keys and values are asked for while the one before is worked on, their places two units before.
+//
+// What bounds it.  One prefix of 32768 keys, 8 key heads of 128, 64 requests of 32 heads (bf16, 134 MB, 34 GFLOP) 74 us: matrix instructions 22 us, vector
+// instructions 23, LDS 17, the start and the pieces (38 MB) 11; without the arithmetic 41 to 54.  4096 keys, 4 key heads, 192 requests of 32 heads 41 us.  Five of 751 to 3001 keys, 6
+// heads of 96, 31 requests (f32, 41 MB) 35 us: six or seven of 32 columns have a query, and the matrix instructions of 32 bits take four times as long.
+// 500 keys, 2 key heads of 64, 4 requests of 8 heads (f16) 7.5 us: the launch, the groups, and ten workgroups' few units one after the other.
 #include "attention.hpp"
 
 #include <algorithm>
@@ -125,7 +134,8 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves
   constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = S::kWide, kChunks = Dim / (4 * kWide), kRow = S::kRow;
   constexpr int kW = Dim / 16, kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;
   constexpr int kTiles = S::kTiles;
-  // weights of f16, 2^14 larger than they are, end at 2^16
+  // weights of f16, 2^14 larger than they are, end at 2^16.  0, every new maximum at once: 8 groups of 128 columns, 4096 keys, 8 key heads of 128 61 us
+  // and 58 this way (bf16), 210 and 195 (f32), 4 groups of 64 columns 73 and 68 (f32).
   constexpr float kSlack = sizeof(T) == 4 ? 5.0f : Kind<T>::kShift ? 1.0f : 8.0f;
   using Frag = Vec<T, kWide>;
   using Part = Vec<T, kPart>;
@@ -442,7 +452,10 @@ template <class T, int Dim, int ColumnWaves> Variant variant() {
   using S = PrefixShape<T, Dim, ColumnWaves>;
   return {&prefix_kernel<T, Dim, ColumnWaves>, (unsigned)S::kColumns, (unsigned)S::kTile};
 }
-// the largest heads leave no registers for waves of other keys
+// A workgroup has 32, 64 or 128 columns, its waves beyond 32 columns each other keys.  As many as groups have on average: what is left empty costs as much as
+// what is not, and more columns read the prefix less often.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
+//   8 of 32 columns 41 / 40 / 48 (bf16), 82 / 114 / 178 (f32);  8 of 64 62 / 43 / 50, 143 / 119 / 183;  8 of 128 108 / 68 / 58, 267 / 223 / 195
+// The largest heads leave no registers for waves of other keys.
 template <class T, int Dim> Variant variant_of_heads(unsigned columns) {
   if constexpr (Dim < 256)
     if (columns <= 32) return variant<T, Dim, 1>();
