@@ -108,8 +108,9 @@ template <class T> __device__ __forceinline__ Vec<T, 4> read_turned(const T *fro
   return __builtin_bit_cast(Vec<T, 4>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Raw *)reinterpret_cast<uintptr_t>(from)));
 }
 
-template <class T, int Dim, int ColumnWaves> struct PrefixShape {
-  static constexpr int kTiles = sizeof(T) == 4 && Dim == 256 ? 1 : 2;        // of 16 columns of a wave, as many as its registers hold
+// Tiles: of 16 columns of a wave
+template <class T, int Dim, int ColumnWaves, int Tiles> struct PrefixShape {
+  static constexpr int kTiles = Tiles;
   static constexpr int kColumns = 16 * kTiles * ColumnWaves, kKeyWaves = kWaves / ColumnWaves;
   static constexpr int kSteps = kKeyWaves == 1 ? 2 : 1, kTile = Kind<T>::kKeys * kKeyWaves * kSteps;
   static constexpr int kWide = 16 / sizeof(T), kRow = Dim / kWide;           // 16 bytes of a key; of them in a row
@@ -128,9 +129,9 @@ template <int Row> __device__ __forceinline__ unsigned place_in_lds(unsigned key
   return key * Row + (chunk ^ turn);
 }
 
-template <class T, int Dim, int ColumnWaves>
-__global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && (ColumnWaves == 1 || sizeof(T) == 4)) ? 1 : 2) void prefix_kernel(PrefixArgs a) {
-  using S = PrefixShape<T, Dim, ColumnWaves>;
+template <class T, int Dim, int ColumnWaves, int Tiles>
+__global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 && (ColumnWaves == 1 || sizeof(T) == 4)) ? 1 : 2) void prefix_kernel(PrefixArgs a) {
+  using S = PrefixShape<T, Dim, ColumnWaves, Tiles>;
   constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = S::kWide, kChunks = Dim / (4 * kWide), kRow = S::kRow;
   constexpr int kW = Dim / 16, kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;
   constexpr int kTiles = S::kTiles;
@@ -448,20 +449,23 @@ struct Variant {
   PrefixKernel kernel;
   unsigned columns, tile;
 };
-template <class T, int Dim, int ColumnWaves> Variant variant() {
-  using S = PrefixShape<T, Dim, ColumnWaves>;
-  return {&prefix_kernel<T, Dim, ColumnWaves>, (unsigned)S::kColumns, (unsigned)S::kTile};
+template <class T, int Dim, int ColumnWaves, int Tiles> Variant variant() {
+  using S = PrefixShape<T, Dim, ColumnWaves, Tiles>;
+  return {&prefix_kernel<T, Dim, ColumnWaves, Tiles>, (unsigned)S::kColumns, (unsigned)S::kTile};
 }
 // A workgroup has 32, 64 or 128 columns, its waves beyond 32 columns each other keys.  As many as groups have on average: what is left empty costs as much as
 // what is not, and more columns read the prefix less often.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
 //   8 of 32 columns 41 / 40 / 48 (bf16), 82 / 114 / 178 (f32);  8 of 64 62 / 43 / 50, 143 / 119 / 183;  8 of 128 108 / 68 / 58, 267 / 223 / 195
 // The largest heads leave no registers for waves of other keys.
 template <class T, int Dim> Variant variant_of_heads(unsigned columns) {
-  if constexpr (Dim < 256)
-    if (columns <= 32) return variant<T, Dim, 1>();
+  constexpr int kMost = sizeof(T) == 4 && Dim == 256 ? 1 : 2;                  // tiles that the registers hold
+  if constexpr (Dim < 256) {
+    if (columns <= 16) return variant<T, Dim, 1, 1>();
+    if (columns <= 32) return variant<T, Dim, 1, kMost>();
+  }
   if constexpr (Dim < 256 || sizeof(T) == 4)
-    if (columns <= 32 * PrefixShape<T, Dim, 2>::kTiles) return variant<T, Dim, 2>();
-  return variant<T, Dim, 4>();
+    if (columns <= 32 * kMost) return variant<T, Dim, 2, kMost>();
+  return variant<T, Dim, 4, kMost>();
 }
 template <class T> Variant variant_of_type(unsigned dim, unsigned columns) {
   return dim <= 64 ? variant_of_heads<T, 64>(columns) : dim <= 128 ? variant_of_heads<T, 128>(columns) : variant_of_heads<T, 256>(columns);
