@@ -1,7 +1,7 @@
 // Attention of requests that share a prefix (include/fc.h, fc_prefix_attention): the keys of the prefix are read once for all of them.
 //
 // The query heads of all requests of a group that read the same key head are columns of one product, 32 of them a wave; a workgroup has
-// `columns` = 32, 64 or 128, its other waves take other keys.  Keys and values of a step go through LDS, which all columns read them from:
+// `columns` = 32, 64 or 128 (16 where there are no more), its other waves take other keys.  Keys and values of a step go through LDS, which all columns read them from:
 //   scores  = K q^T, outputs = V^T p^T, as in attention.hpp: lane (r, g), r = lane % 16, g = lane / 16, has columns r and 16 + r and the
 //   keys 4g .. 4g+3 of every 16, in whose order the values' product takes them from LDS.
 // What a workgroup has of a row (prefix.hpp) is written as it is: the attention of the requests' own keys, which follows, joins it.
@@ -12,8 +12,9 @@
 //
 // What bounds it.  One prefix of 32768 keys, 8 key heads of 128, 64 requests of 32 heads (bf16, 134 MB, 34 GFLOP) 74 us: matrix instructions 22 us, vector
 // instructions 23, LDS 17, the start and the pieces (38 MB) 11; without the arithmetic 41 to 54.  4096 keys, 4 key heads, 192 requests of 32 heads 41 us.  Five of 751 to 3001 keys, 6
-// heads of 96, 31 requests (f32, 41 MB) 35 us: six or seven of 32 columns have a query, and the matrix instructions of 32 bits take four times as long.
-// 500 keys, 2 key heads of 64, 4 requests of 8 heads (f16) 7.5 us: the launch, the groups, and ten workgroups' few units one after the other.
+// heads of 96, 31 requests (f32, 41 MB) 26.5 us: six or seven of 16 columns have a query, and the matrix instructions of 32 bits take four times as long; two
+// workgroups a compute unit instead of one gain nothing.
+// 500 keys, 2 key heads of 64, 4 requests of 8 heads (f16) 6.4 us: the launch, the groups, then pages, keys and products one after the other.
 #include "attention.hpp"
 
 #include <algorithm>
@@ -453,8 +454,8 @@ template <class T, int Dim, int ColumnWaves, int Tiles> Variant variant() {
   using S = PrefixShape<T, Dim, ColumnWaves, Tiles>;
   return {&prefix_kernel<T, Dim, ColumnWaves, Tiles>, (unsigned)S::kColumns, (unsigned)S::kTile};
 }
-// A workgroup has 32, 64 or 128 columns, its waves beyond 32 columns each other keys.  As many as groups have on average: what is left empty costs as much as
-// what is not, and more columns read the prefix less often.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
+// As many columns as groups have on average: what is left empty costs as much as what is not, and more columns read the prefix less often.  16 instead of 32:
+// 6 requests of a head a key head (f32) 26.5 us and 35, 4 of four (f16) 6.4 and 7.5.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
 //   8 of 32 columns 41 / 40 / 48 (bf16), 82 / 114 / 178 (f32);  8 of 64 62 / 43 / 50, 143 / 119 / 183;  8 of 128 108 / 68 / 58, 267 / 223 / 195
 // The largest heads leave no registers for waves of other keys.
 template <class T, int Dim> Variant variant_of_heads(unsigned columns) {
