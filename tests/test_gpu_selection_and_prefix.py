@@ -206,6 +206,18 @@ def test_selection_for_many_requests(width):
     check_select(select_case(lengths, 2, 2, 16, 4, 7, "f16", seed=width), 4)
 
 
+@pytest.mark.parametrize("dtype,hq,hk,width", [("bf16", 2, 1, 100), ("f32", 1, 1, 700), ("f16", 5, 1, 2100), ("bf16", 3, 3, 65)])
+def test_selection_of_rows_in_pieces_for_more_requests_than_a_workgroup_has_threads(dtype, hq, hk, width):
+    rng = np.random.default_rng(width)
+    lengths = rng.integers(0, 150, 300)
+    lengths[::41] = 4 * rng.integers(1, width + 1, lengths[::41].shape)
+    lengths[[0, 256, 299]] = 4 * width, 4 * width - 3, 4 * width
+    s = select_case(lengths, hq, hk, 24, 4, 7, dtype, seed=width)
+    check_select(s, 4)
+    s["selected"].fill_(5), s["selected_lengths"].fill_(5)   # again in the same arrays
+    check_select(s, 4)
+
+
 def test_equal_scores_go_to_the_first_pages():
     for fill in (0.0, 1.5):
         s = select_case([700, 513, 16], 2, 2, 64, 8, 9, "bf16", seed=1)
@@ -406,6 +418,13 @@ def test_prefixes_that_are_long_or_many(dtype):
     check_prefix(prefix_case([(70, 900)], [3] * 70, 8, 2, 128, 16, dtype, seed=2), dtype)
     check_prefix(prefix_case([(2, n % 50) for n in range(150)], [n % 9 for n in range(310)], 4, 2, 64, 8, dtype, seed=3), dtype)
     check_prefix(prefix_case([(1, 5)] * 1024, [2] * 1030, 2, 1, 16, 8, dtype, seed=4), dtype)
+
+
+@pytest.mark.parametrize("dtype,dim", [("f32", 40), ("f32", 128), ("f16", 64), ("bf16", 128), ("bf16", 96), ("f32", 256), ("f16", 256)])
+def test_a_large_group_among_small_ones(dtype, dim):
+    # as many columns as a small group has on average, and many times as many in one group
+    groups = [(1, 70)] * 15 + [(40, 333)] + [(1, 129)] * 15
+    check_prefix(prefix_case(groups, np.arange(75) % 23, 4, 1, dim, 8, dtype, seed=dim), dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
