@@ -21,10 +21,12 @@ namespace fc {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+// Threads of a workgroup.  Many: where rows of very many pages are split, of which one workgroup orders all scores: one request of 8192 pages, 8 key heads 34 us and
+// 44 by few, of 4096 31 and 30; short rows leave their waves idle (8 requests of 500 pages 26 and 16).
+constexpr int kFew = 256, kMany = 1024;
 // of 16 pages, that a wave reads before it scores them: two take 67 us where one takes 61 (64 ragged requests), 15.4 and 12.5 (19 in f32)
 constexpr int kTilesOfWave = 1;
-constexpr unsigned kBlockPages = 16 * kTilesOfWave * kWaves; // of a row that a workgroup scores at a time
+constexpr unsigned block_pages(int threads) { return 16 * kTilesOfWave * threads / kWave; }       // of a row that a workgroup scores at a time
 constexpr unsigned kKept = 1024;                             // keys that stay in LDS where one workgroup has a whole row (300 requests of 900 pages 245 us, 264 by memory)
 constexpr unsigned kListed = 2048;                           // selected positions that are put in order in LDS
 constexpr unsigned long long kAlways = ~0ull;                // above every score; 0, below every score, is a page that is not there
@@ -186,12 +188,12 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, unsigned all) 
 struct Sums {
   unsigned x, y, all_x, all_y;
 };
-__device__ __forceinline__ Sums sum_of_waves(unsigned x, unsigned y, unsigned (*lds)[2]) {
+template <int Waves> __device__ __forceinline__ Sums sum_of_waves(unsigned x, unsigned y, unsigned (*lds)[2]) {
   if (lane_id() == 0) { lds[wave_id()][0] = x; lds[wave_id()][1] = y; }
   __syncthreads();
   Sums s{0, 0, 0, 0};
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < Waves; ++w) {
     if (w < wave_id()) { s.x += lds[w][0]; s.y += lds[w][1]; }
     s.all_x += lds[w][0];
     s.all_y += lds[w][1];
@@ -206,15 +208,17 @@ __device__ __forceinline__ unsigned length_of(const SelectArgs &a, int length) {
 __device__ __forceinline__ unsigned pages_of(const SelectArgs &a, unsigned length) { return (length + a.page - 1) / a.page; }
 // no more pages than are wanted: all that are there are taken
 __device__ __forceinline__ bool is_scored(const SelectArgs &a, unsigned count) { return count > a.most && a.pages > 0; }
-// of a row: kBlockPages pages that are scored, or one
-__device__ __forceinline__ unsigned units_of(const SelectArgs &a, unsigned count) { return is_scored(a, count) ? (count + kBlockPages - 1) / kBlockPages : 1u; }
+// of a row: as many pages as a workgroup scores at a time, or one
+template <int Threads> __device__ __forceinline__ unsigned units_of(const SelectArgs &a, unsigned count) { return is_scored(a, count) ? (count - 1) / block_pages(Threads) + 1 : 1u; }
 
 // Scores the units [unit0, unit1) of the row of request b and key head `head`; the last of the `parts` workgroups that it is split over, who count on
 // `counter`, then selects.
 // Held: keys of a row that a lane keeps in registers, no more than a call's tables need; 0: as many as there are, read again whenever they are looked at
 // (one request of 8192 pages 50 us with its keys held and 65 without; 32 of 2000 pages 106, 112 without, 118 with registers for four times as many).
-template <class T, int HeadTiles, bool Whole, int Held>
+template <class T, int HeadTiles, bool Whole, int Held, int Threads>
 __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, unsigned head, unsigned length, unsigned unit0, unsigned unit1, unsigned parts, unsigned *counter) {
+  constexpr int kWaves = Threads / kWave;
+  constexpr unsigned kBlock = block_pages(Threads);
   __shared__ unsigned long long kept[kKept];
   __shared__ unsigned counts[2][256], sums[2][kWaves][2], found[2][3];
   __shared__ int ends[2][kWaves];
@@ -226,13 +230,13 @@ __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, u
   const bool scored = is_scored(a, count);
   const bool near = parts == 1 && count <= kKept;            // the keys never leave LDS
   // a wave has `each` times 64 positions side by side, a lane one of every 64
-  const unsigned each = (count + kThreads - 1) / kThreads, w0 = (unsigned)wave_id() * each * kWave + lane_id();
+  const unsigned each = (count + Threads - 1) / Threads, w0 = (unsigned)wave_id() * each * kWave + lane_id();
   if (scored) {
     const T *const q = reinterpret_cast<const T *>(a.q) + b * a.q_request + head * a.group * a.q_head;
     const T *const bounds = reinterpret_cast<const T *>(a.bounds) + head * a.b_head;
     Scores<T, HeadTiles, Whole> scores(a, q, bounds, table);
-    for (unsigned at = unit0 * kBlockPages; at < min(unit1 * kBlockPages, count); at += kBlockPages)
-      scores.run(at + kBlockPages / kWaves * (unsigned)wave_id(), min(at + kBlockPages, count), [&](unsigned w, bool there, double s, bool first) {
+    for (unsigned at = unit0 * kBlock; at < min(unit1 * kBlock, count); at += kBlock)
+      scores.run(at + kBlock / kWaves * (unsigned)wave_id(), min(at + kBlock, count), [&](unsigned w, bool there, double s, bool first) {
         unsigned long long key = !there ? 0ull : w < a.first || w + a.last >= count ? kAlways : key_of(s);
         if (near) kept[w] = first ? key : max(kept[w], key);
         else {
@@ -308,8 +312,8 @@ __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, u
     least = wave_reduce<MaxI32>(least);
     largest = wave_reduce<MaxI32>(largest);
     if (lane_id() == 0) { ends[0][wave_id()] = least; ends[1][wave_id()] = largest; }
-    counts[0][threadIdx.x] = 0;
-    const Sums there = sum_of_waves(mine, always, sums[turn]);
+    if (threadIdx.x < 256) counts[0][threadIdx.x] = 0;
+    const Sums there = sum_of_waves<kWaves>(mine, always, sums[turn]);
     turn ^= 1;
     all = there.all_x <= a.most;
     const unsigned wanted = a.most - min(there.all_y, a.most);                 // of those that are not taken anyway
@@ -360,7 +364,7 @@ __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, u
     above += lanes_of(over);
     at_bar += lanes_of(!over && key != 0 && key >= low);
   });
-  const Sums to = sum_of_waves(above, at_bar, sums[turn]);
+  const Sums to = sum_of_waves<kWaves>(above, at_bar, sums[turn]);
   unsigned at_before = to.y, slot0 = to.x + min(at_before, level);
   const unsigned taken = min(to.all_x + min(to.all_y, level), a.most);
   bool is_last = false;
@@ -380,23 +384,24 @@ __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, u
     slot0 += (unsigned)__popcll(mask);
   });
   const unsigned short_of = __syncthreads_or(is_last) ? count * a.page - length : 0u;
-  for (unsigned k = threadIdx.x; k < min(taken, kListed); k += kThreads) selected[k] = table[listed[k]];
-  for (unsigned k = taken + threadIdx.x; k < a.most; k += kThreads) selected[k] = -1;
+  for (unsigned k = threadIdx.x; k < min(taken, kListed); k += Threads) selected[k] = table[listed[k]];
+  for (unsigned k = taken + threadIdx.x; k < a.most; k += Threads) selected[k] = -1;
   if (threadIdx.x == 0) a.selected_lengths[b * a.l_request + head] = (int)(taken * a.page - short_of);
 }
 
-template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+template <class T, int HeadTiles, bool Whole, int Held, int Threads> __global__ __launch_bounds__(Threads) void select_kernel(SelectArgs a) {
+  constexpr int kWaves = Threads / kWave;
   unsigned b, length, units, unit0 = 0, unit1, parts = 1, head;
   if (a.pieces == 0) {
     b = blockIdx.x / a.heads;
     head = blockIdx.x - b * a.heads;
     length = length_of(a, load_scalar(a.lengths + b));
-    unit1 = units_of(a, pages_of(a, length));
+    unit1 = units_of<Threads>(a, pages_of(a, length));
   } else {
-    __shared__ unsigned ends[kThreads], sums[2][kWaves];     // pieces of the rows of a thread's requests, summed up to it
-    const unsigned each = (a.requests + kThreads - 1) / kThreads, b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
+    __shared__ unsigned ends[Threads], sums[2][kWaves];     // pieces of the rows of a thread's requests, summed up to it
+    const unsigned each = (a.requests + Threads - 1) / Threads, b0 = min(threadIdx.x * each, a.requests), b1 = min(b0 + each, a.requests);
     unsigned mine = 0;
-    for (unsigned i = b0; i < b1; ++i) mine += units_of(a, pages_of(a, length_of(a, a.lengths[i]))) * a.heads;
+    for (unsigned i = b0; i < b1; ++i) mine += units_of<Threads>(a, pages_of(a, length_of(a, a.lengths[i]))) * a.heads;
     mine = (unsigned)wave_reduce<AddI32>((int)mine);
     if (lane_id() == 0) sums[0][wave_id()] = mine;
     __syncthreads();
@@ -406,7 +411,7 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
     const unsigned share = max((total + a.pieces - 1) / a.pieces, 1u);
     auto parts_of = [&](unsigned n) { return (n + share - 1) / share; };
     mine = 0;
-    for (unsigned i = b0; i < b1; ++i) mine += parts_of(units_of(a, pages_of(a, length_of(a, a.lengths[i])))) * a.heads;
+    for (unsigned i = b0; i < b1; ++i) mine += parts_of(units_of<Threads>(a, pages_of(a, length_of(a, a.lengths[i])))) * a.heads;
     const unsigned upto = (unsigned)wave_scan_inclusive<AddI32>((int)mine);
     if (lane_id() == kWave - 1) sums[1][wave_id()] = upto;
     __syncthreads();
@@ -416,16 +421,16 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
       if (w < wave_id()) before += sums[1][w];
     ends[threadIdx.x] = before + upto;
     __syncthreads();
-    if (blockIdx.x >= ends[kThreads - 1]) return;
+    if (blockIdx.x >= ends[Threads - 1]) return;
     // the request of this piece, and the pieces before it
     unsigned chunk = 0;
 #pragma unroll
-    for (int k = 0; k < kThreads / kWave; ++k) chunk += (unsigned)__popcll(__ballot(ends[k * kWave + lane_id()] <= blockIdx.x));
+    for (int k = 0; k < Threads / kWave; ++k) chunk += (unsigned)__popcll(__ballot(ends[k * kWave + lane_id()] <= blockIdx.x));
     chunk = __builtin_amdgcn_readfirstlane(chunk);
     before = chunk ? __builtin_amdgcn_readfirstlane(ends[chunk - 1]) : 0u;
     for (b = chunk * each;; ++b) {
       length = length_of(a, load_scalar(a.lengths + b));
-      units = units_of(a, pages_of(a, length));
+      units = units_of<Threads>(a, pages_of(a, length));
       parts = parts_of(units);
       if (blockIdx.x - before < parts * a.heads) break;
       before += parts * a.heads;
@@ -435,26 +440,32 @@ template <class T, int HeadTiles, bool Whole, int Held> __global__ __launch_boun
     unit0 = (unsigned)((unsigned long long)units * part / parts);
     unit1 = (unsigned)((unsigned long long)units * (part + 1) / parts);
   }
-  select_of_row<T, HeadTiles, Whole, Held>(a, b, head, length, unit0, unit1, parts, a.counters + (parts > 1 ? b * a.heads + head : 0));
+  select_of_row<T, HeadTiles, Whole, Held, Threads>(a, b, head, length, unit0, unit1, parts, a.counters + (parts > 1 ? b * a.heads + head : 0));
 }
 
 // With more rows than half of these, each has a workgroup.  Pieces: as many as workgroups are resident; half of them take 60 us where these take 56 (64 ragged
 // requests), twice as many 57, a fixed number of pieces for every row 61.
 constexpr unsigned kWorkgroups = 2048;
+constexpr unsigned kLongRow = 4 * kMany;                     // pages; longer ones by many threads
 
 struct PageSelect final : Operator {
   SelectArgs a{};
   int32_t dtype;
   bool far = false;                        // keys leave LDS
+  int threads = kFew;
   template <class F> void with_kernel(F &&f) const {
     auto by_width = [&](auto t, auto tiles, auto whole) {
       using T = decltype(t);
       constexpr int kTiles = decltype(tiles)::value;
       constexpr bool kWhole = decltype(whole)::value;
-      if (a.width <= 4 * kThreads) f(&select_kernel<T, kTiles, kWhole, 4>);
-      else if (a.width <= 8 * kThreads) f(&select_kernel<T, kTiles, kWhole, 8>);
-      else if (a.width <= 32 * kThreads) f(&select_kernel<T, kTiles, kWhole, 32>);
-      else f(&select_kernel<T, kTiles, kWhole, 0>);
+      if (threads == kMany) {
+        constexpr int kOfMany = kWhole ? kTiles : 1;           // two with the tests do not fit the registers
+        if (a.width <= 8 * kMany) f(&select_kernel<T, kOfMany, kWhole, 8, kMany>);
+        else f(&select_kernel<T, kOfMany, kWhole, 0, kMany>);
+      } else if (a.width <= 4 * kFew) f(&select_kernel<T, kTiles, kWhole, 4, kFew>);
+      else if (a.width <= 8 * kFew) f(&select_kernel<T, kTiles, kWhole, 8, kFew>);
+      else if (a.width <= 32 * kFew) f(&select_kernel<T, kTiles, kWhole, 32, kFew>);
+      else f(&select_kernel<T, kTiles, kWhole, 0, kFew>);
     };
     auto by_dim = [&](auto t, auto tiles) {
       if (a.dim % (64 / sizeof(t)) == 0) by_width(t, tiles, std::true_type{});
@@ -474,7 +485,7 @@ struct PageSelect final : Operator {
     SelectArgs args = a;
     args.keys = far ? reinterpret_cast<unsigned long long *>(r.workspace) : nullptr;
     args.counters = r.counters;
-    with_kernel([&](auto kernel) { r.launch(kernel, a.pieces + a.requests * a.heads, kThreads, args); });
+    with_kernel([&](auto kernel) { r.launch(kernel, a.pieces + a.requests * a.heads, threads, args); });
   }
   const char *name() const override { return "page select"; }
 };
@@ -534,14 +545,14 @@ int make_page_select(const fc_page_select &n, std::unique_ptr<Operator> &out, st
   // no more than the pages of a request of 2^31-1 keys are looked at
   a.width = (unsigned)std::min<uint64_t>(width, (0x7fffffffu + (uint64_t)a.page - 1) / a.page);
   const unsigned rows = a.requests * a.heads;
-  const unsigned units = std::max(1u, ceil_div(a.width, kBlockPages));
-  const bool split = rows <= kWorkgroups / 2 && units > 1;
+  const bool split = rows <= kWorkgroups / 2 && a.width > block_pages(kFew);
+  if (split && a.width > kLongRow) op->threads = kMany;
   op->far = a.width > kKept || split;
   if ((uint64_t)rows * a.width > (uint64_t)1 << 36) return c.fail(FC_E_LIMIT, "too many requests, heads and pages of a request together").code();
   if (split) {
     unsigned resident = 0;
-    op->with_kernel([&](auto kernel) { resident = resident_workgroups(kernel, kThreads); });
-    a.pieces = std::min(resident ? resident : 1024u, rows * units);
+    op->with_kernel([&](auto kernel) { resident = resident_workgroups(kernel, op->threads); });
+    a.pieces = std::min(resident ? resident : 256u, rows * ceil_div(a.width, block_pages(op->threads)));
   }
   out = std::move(op);
   return FC_OK;
