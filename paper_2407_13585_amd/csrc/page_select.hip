@@ -9,8 +9,8 @@
 // for a request and key head (a row); where rows are few and their pages many, a row's scores are split into pieces of about the same size, and the last
 // workgroup to be done selects.
 //
-// What bounds it.  One request of 4096 pages of 8 key heads of 128, 64 heads (bf16, 17 MB) 30 us: 5 to the row's workgroup and its table, 8 for the scores
-// (reads 4, arithmetic 4, each once and one behind the other), 3 to hand them to one workgroup, 13 of that workgroup alone for 16 keys a lane.  64 requests of up to 1024 pages, 8
+// What bounds it.  One request of 4096 pages of 8 key heads of 128, 64 heads (bf16, 17 MB) 28 us: 5 to the row's workgroup and its table, 8 for the scores
+// (reads 4, arithmetic 4, each once and one behind the other), 3 to hand them to one workgroup, the rest that workgroup alone, step after step.  64 requests of up to 1024 pages, 8
 // key heads of 128, 32 heads (bf16, 134 MB) 56 us: without selection 48.5, without most of the arithmetic too 42.5, without the table's reads 35, so
 // 3.8 TB/s of what it must read; 300 requests of 900 pages (bf16, 1.1 GB) 250 us, 4.4 TB/s, in 32 bits 442 us, 5.0 TB/s.  4 short requests 3.8 us: the launch.
 #include "operators.hpp"
@@ -21,8 +21,9 @@ namespace fc {
 
 namespace {
 
-// Threads of a workgroup.  Many: where rows of very many pages are split, of which one workgroup orders all scores: one request of 8192 pages, 8 key heads 34 us and
-// 44 by few, of 4096 31 and 30; short rows leave their waves idle (8 requests of 500 pages 26 and 16).
+// Threads of a workgroup.  Many: where long rows are split, of which one workgroup orders all scores.  us by many and by few, 8 key heads of 128, groups of 8 (bf16): one
+// request of 2100 pages 28.5 and 27.6, of 3000 28.9 and 31.1, of 6000 31 and 39, of 16000 66 and 118; 32 requests of 2100 pages 106 and 119, of 6000 276 and
+// 300.  Short rows leave their waves idle: 8 requests of 500 pages 26 and 16, 64 of 1024 78 and 68.
 constexpr int kFew = 256, kMany = 1024;
 // of 16 pages, that a wave reads before it scores them: two take 67 us where one takes 61 (64 ragged requests), 15.4 and 12.5 (19 in f32)
 constexpr int kTilesOfWave = 1;
@@ -214,7 +215,7 @@ template <int Threads> __device__ __forceinline__ unsigned units_of(const Select
 // Scores the units [unit0, unit1) of the row of request b and key head `head`; the last of the `parts` workgroups that it is split over, who count on
 // `counter`, then selects.
 // Held: keys of a row that a lane keeps in registers, no more than a call's tables need; 0: as many as there are, read again whenever they are looked at
-// (one request of 8192 pages 50 us with its keys held and 65 without; 32 of 2000 pages 106, 112 without, 118 with registers for four times as many).
+// (32 requests of 2000 pages 106 us, 112 without, 118 with registers for four times as many).
 template <class T, int HeadTiles, bool Whole, int Held, int Threads>
 __device__ __forceinline__ void select_of_row(const SelectArgs &a, unsigned b, unsigned head, unsigned length, unsigned unit0, unsigned unit1, unsigned parts, unsigned *counter) {
   constexpr int kWaves = Threads / kWave;
@@ -446,7 +447,7 @@ template <class T, int HeadTiles, bool Whole, int Held, int Threads> __global__ 
 // With more rows than half of these, each has a workgroup.  Pieces: as many as workgroups are resident; half of them take 60 us where these take 56 (64 ragged
 // requests), twice as many 57, a fixed number of pieces for every row 61.
 constexpr unsigned kWorkgroups = 2048;
-constexpr unsigned kLongRow = 4 * kMany;                     // pages; longer ones by many threads
+constexpr unsigned kLongRow = 2 * kMany;                     // pages; longer ones by many threads
 
 struct PageSelect final : Operator {
   SelectArgs a{};
