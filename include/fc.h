@@ -474,7 +474,7 @@ typedef struct fc_page_select {
  * before group_start[0] and from group_start[G] on have no prefix.  A start below an earlier one counts as that one, below 0 as 0, above B as B.  Request
  * b's own keys are the lengths[b] keys on the pages table[b].  The result is that of fc_paged_attention without a window over both, each key
  * of a prefix read once for 16 to 128 of the query heads that see it.  A request may have no keys of its own, a group no prefix.
- * scale is below 2^126 (FC_E_UNSUPPORTED); scores of f16 and bf16 beyond 2^127 either way may count as infinite.  At most 1024 groups; pieces of a prefix (32 keys of a key head for 128 query heads, at least) are counted in 31 bits, of as many keys as its
+ * scale is below 2^126 (FC_E_UNSUPPORTED).  At most 1024 groups; pieces of a prefix (32 keys of a key head for 128 query heads, at least) are counted in 31 bits, of as many keys as its
  * table could hold (FC_E_LIMIT). */
 typedef struct fc_prefix_attention {
   fc_tensor q;               /* as in fc_paged_attention */

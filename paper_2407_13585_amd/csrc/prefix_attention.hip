@@ -168,9 +168,12 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
   const unsigned r = lane_id() & 15, g4 = lane_id() >> 4;
   const unsigned wave = uniform((unsigned)wave_id()), column_wave = wave % ColumnWaves, key_wave = wave / ColumnWaves;
   const T *const q0 = reinterpret_cast<const T *>(a.q);
-  // 16 bits: what takes a product of q and k to the power of 2 that its weight is; m is such a power until the piece is written
-  const float by = sizeof(T) == 4 ? 1.0f : a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
-  auto power = [](float x) { return sizeof(T) == 4 ? exp_of(x) : __builtin_amdgcn_exp2f(x); };
+  // 16 bits: m is half a product of q and k until the piece is written, and `by` takes differences of such halves to powers of 2.  A difference is taken
+  // first, so that the largest key's is 0 whatever its product is: the rounding of a large product times `by` would be many powers of 2.  The
+  // difference of two products need not be a finite number of 32 bits where its power of 2 is; that of their halves is one.
+  constexpr float kOfProduct = sizeof(T) == 4 ? 1.0f : 0.5f;
+  const float by = sizeof(T) == 4 ? 1.0f : a.scale == 0.0f ? 1.0f : fabsf(a.scale) * (kLog2e / kOfProduct);
+  auto power = [by](float x) { return sizeof(T) == 4 ? exp_of(x) : __builtin_amdgcn_exp2f(x * by); };
   unsigned at = (unsigned)min((unsigned long long)blockIdx.x * share, (unsigned long long)total);
   const unsigned end = min(at + share, total);
   while (at < end) {
@@ -320,10 +323,9 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
           for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, p[t][u][i]);
-          // m may stay behind the largest score by kSlack, so that sums are seldom multiplied.  16 bits: m in powers of 2, and one multiplication
-          // that is not rounded takes a product to the exponent of its weight.
-          most *= by;
-          if (__any(most > m[t] + kSlack)) {
+          // m may stay behind the largest score by kSlack, so that sums are seldom multiplied
+          most *= kOfProduct;
+          if (__any((most - m[t]) * by > kSlack)) {
             most = fmaxf(column_max(most), m[t]);
             const float keep = most == -__builtin_inff() ? 1.0f : power(m[t] - most);
             m[t] = most;
@@ -332,12 +334,11 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
             for (int j = 0; j < kW; ++j) o[t][j] *= keep;
           }
           const float top = m[t] == -__builtin_inff() ? 0.0f : m[t];
-          const float off = (float)Kind<T>::kShift - top;
 #pragma unroll
           for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              p[t][u][i] = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(fmaf(p[t][u][i], by, off)) : exp_of(p[t][u][i] - top);
+              p[t][u][i] = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(fmaf(fmaf(p[t][u][i], kOfProduct, -top), by, (float)Kind<T>::kShift)) : exp_of(p[t][u][i] - top);
               l[t] += p[t][u][i];
             }
         }
@@ -438,7 +439,8 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
           if (d < a.dim) store_vec<float, 4>(piece + (size_t)(first + column) * a.dim + d, *reinterpret_cast<const Vec<float, 4> *>(rows + column * (Dim + 4) + d));
         }
         __builtin_amdgcn_wave_barrier();
-        if (g4 == 0 && r < live) store_vec<float, 2>(piece + (size_t)S::kColumns * a.dim + 2 * (first + r), Vec<float, 2>{sizeof(T) == 4 ? m[t] : m[t] * kLn2, sum});
+        const float top = sizeof(T) == 4 || m[t] == -__builtin_inff() ? m[t] : m[t] * (fabsf(a.scale) / kOfProduct);          // a score, rounded as in attention.hpp
+        if (g4 == 0 && r < live) store_vec<float, 2>(piece + (size_t)S::kColumns * a.dim + 2 * (first + r), Vec<float, 2>{top, sum});
       }
     }
     at += unit1 - unit0;
