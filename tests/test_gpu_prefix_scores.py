@@ -13,7 +13,7 @@ import pytest
 
 from oracle import cache as O
 from test_gpu_operators import TINY, U, gpu, host, near
-from test_gpu_selection_and_prefix import ORDER, attended, prefix_case
+from test_gpu_selection_and_prefix import ORDER, attended, check_prefix, prefix_case
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +115,14 @@ def test_scores_beyond_32_bits_are_infinite_as_without_a_prefix(scale):
             assert np.isnan(out).all() and np.isnan(lse).all()
         else:                                                # all are -inf: as no keys
             assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_a_scale_of_zero_over_prefixes_of_which_nothing_is_there(dtype):
+    # every score is 0, so out is the mean of the values that are there, and lse the logarithm of their number
+    s = prefix_case([(3, 100), (3, 64), (2, 40)], [0, 5, 40, 0, 7, 64, 0, 3, 9], 8, 2, 64, PAGE, dtype, seed=6)
+    table = host(s["prefix_table"]).copy()
+    table[0, :], table[2, 1] = -1, 2 ** 31 - 1
+    s["prefix_table"] = gpu(table)
+    check_prefix(s, dtype, scale=0.0)
+    check_prefix(s, dtype, scale=-0.0)
