@@ -437,7 +437,7 @@ typedef struct fc_paged_attention {
  * lengths[b]-1 (and below W P), which lie where fc_paged_attention finds them.  For each page that holds any, and each key head:
  *   bounds[page][h][0] = the least, bounds[page][h][1] = the largest of every element of its new keys, and of what was there before where
  *   the page's first position is below lengths_before[b].
- * A NaN among the keys makes a NaN of both.  Pages outside the cache are left out; a page takes new keys of one request only.  Keys that a request drops from its end
+ * A NaN among the keys makes a NaN of both.  Pages outside the cache are left out; a page takes new keys of one request only, at one place of its table.  Keys that a request drops from its end
  * leave bounds that are still bounds.  A step that is run again gives the same.  Pages of a request that can have new keys times heads: 2^31-1 of all
  * requests together (FC_E_LIMIT). */
 typedef struct fc_page_bounds {
@@ -456,7 +456,8 @@ typedef struct fc_page_bounds {
  * what is newest), and of the others those of the largest scores, of equal ones those that come first, S in all; all that are there where they are no more.
  * selected[b][h]: their numbers in the order of the table, -1 behind them.  selected_lengths[b][h]: the keys they hold, which is P each but for
  * the last page of the request.  Both are what fc_paged_attention takes as a table of rank 3 and its lengths.
- * S P is at most 2^31-1, B Hk 2^24-1, B Hk times the pages of a request 2^36 (FC_E_LIMIT). */
+ * S P is at most 2^31-1, B Hk 2^24-1, B Hk times the pages of a request 2^36 (FC_E_LIMIT).  How rows are spread over the device goes by W: a table much
+ * wider than its requests are long costs time. */
 typedef struct fc_page_select {
   fc_tensor q;                 /* [B, Hq, D]: f32, f16 or bf16; D a multiple of 8, at most 256; rows 16-byte aligned */
   fc_tensor bounds;            /* [pages, Hk, 2, D] of the same type; rows 16-byte aligned */
@@ -475,7 +476,8 @@ typedef struct fc_page_select {
  * b's own keys are the lengths[b] keys on the pages table[b].  The result is that of fc_paged_attention without a window over both, each key
  * of a prefix read once for 16 to 128 of the query heads that see it.  A request may have no keys of its own, a group no prefix.
  * scale is below 2^126 (FC_E_UNSUPPORTED).  At most 1024 groups; pieces of a prefix (32 keys of a key head for 128 query heads, at least) are counted in 31 bits, of as many keys as its
- * table could hold (FC_E_LIMIT). */
+ * table could hold (FC_E_LIMIT).  How many query heads read a prefix together goes by B Hq / (Hk G): places for groups that have no requests, and many requests
+ * without a group, cost time. */
 typedef struct fc_prefix_attention {
   fc_tensor q;               /* as in fc_paged_attention */
   fc_tensor k_cache;

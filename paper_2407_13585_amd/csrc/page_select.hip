@@ -23,7 +23,9 @@ namespace {
 
 // Threads of a workgroup.  Many: where long rows are split, of which one workgroup orders all scores.  us by many and by few, 8 key heads of 128, groups of 8 (bf16): one
 // request of 2100 pages 28.5 and 27.6, of 3000 28.9 and 31.1, of 6000 31 and 39, of 16000 66 and 118; 32 requests of 2100 pages 106 and 119, of 6000 276 and
-// 300.  Short rows leave their waves idle: 8 requests of 500 pages 26 and 16, 64 of 1024 78 and 68.
+// 300.  Short rows leave their waves idle: 8 requests of 500 pages 26 and 16, 64 of 1024 78 and 68.  The width of the table decides, since lengths lie on the device: a table
+// that is much wider than its requests are long costs what this says.  Widths of 2048 entries at most and of more: 8 requests of 500 pages, groups of 8, 17 and 24.5
+// us, 64 of 1 to 1024 pages, groups of 4, 56 and 78, 64 of 16 pages 3.6 (17 entries) and 15 (4097).
 constexpr int kFew = 256, kMany = 1024;
 // of 16 pages, that a wave reads before it scores them: two take 67 us where one takes 61 (64 ragged requests), 15.4 and 12.5 (19 in f32)
 constexpr int kTilesOfWave = 1;

@@ -6,14 +6,14 @@
 //   keys 4g .. 4g+3 of every 16, in whose order the values' product takes them from LDS.
 // What a workgroup has of a row (prefix.hpp) is written as it is: the attention of the requests' own keys, which follows, joins it.
 //
-// A step of 32 keys (16 of 32 bits) costs a wave 2 * 4 products for the scores and 3 * 8 for the values (128 elements of 16 bits), about 6 vector
-// instructions for each of its 16 scores a lane, and 16 kB from LDS; the three add up, since all waves of a workgroup come to each of them at about the same time.
+// A step of 32 keys (16 of 32 bits) and 32 columns costs a wave 2 * 8 products for the scores and 2 * 16 for the values (128 elements of 16 bits, weights in two
+// parts), nine to ten vector instructions for each of its 16 scores a lane, and 16 kB from LDS; the three add up, since all waves of a workgroup come to each of them at about the same time.
 // A unit's keys and values are asked for while the one before is worked on, their places two units before.
 //
-// What bounds it.  One prefix of 32768 keys, 8 key heads of 128, 64 requests of 32 heads (bf16, 134 MB, 34 GFLOP) 74 us: matrix instructions 22 us, vector
-// instructions 23, LDS 17, the start and the pieces (38 MB) 11; without the arithmetic 41 to 54.  4096 keys, 4 key heads, 192 requests of 32 heads 41 us.  Five of 751 to 3001 keys, 6
-// heads of 96, 31 requests (f32, 41 MB) 26.5 us: six or seven of 16 columns have a query, and the matrix instructions of 32 bits take four times as long; two
-// workgroups a compute unit instead of one gain nothing.
+// What bounds it.  One prefix of 32768 keys, 8 key heads of 128, 64 requests of 32 heads (bf16, 134 MB, 34 GFLOP) 76 us: matrix instructions 22 us, vector
+// instructions 25, LDS 17, the start and the pieces (38 MB) 11; without the arithmetic 41 to 54.  4096 keys, 4 key heads, 192 requests of 32 heads 42 us.  Five of 1501 to 3001 keys, 6
+// heads of 96, 31 requests (f32, 55 MB) 26.5 us: six or seven of 16 columns have a query, and a matrix instruction of 32 bits has an eighth of the products of one of 16
+// bits and takes twice as long (32 cycles and 16); two workgroups a compute unit instead of one gain nothing.
 // 500 keys, 2 key heads of 64, 4 requests of 8 heads (f16) 6.4 us: the launch, the groups, then pages, keys and products one after the other.
 #include "attention.hpp"
 
@@ -136,8 +136,8 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
   constexpr int kKeys = Kind<T>::kKeys, kSub = kKeys / 16, kWide = S::kWide, kChunks = Dim / (4 * kWide), kRow = S::kRow;
   constexpr int kW = Dim / 16, kParts = kW < kWide ? 1 : kW / kWide, kPart = kW < kWide ? kW : kWide;
   constexpr int kTiles = S::kTiles;
-  // weights of f16, 2^14 larger than they are, end at 2^16.  0, every new maximum at once: 8 groups of 128 columns, 4096 keys, 8 key heads of 128 61 us
-  // and 58 this way (bf16), 210 and 195 (f32), 4 groups of 64 columns 73 and 68 (f32).
+  // weights of f16, 2^14 larger than they are, end at 2^16.  0, every new maximum at once: 8 groups of 128 columns, 4096 keys, 8 key heads of 128 63 us
+  // and 60 this way (bf16), 210 and 196 (f32), 4 groups of 64 columns 73 and 68 (f32).
   constexpr float kSlack = sizeof(T) == 4 ? 5.0f : Kind<T>::kShift ? 1.0f : 8.0f;
   using Frag = Vec<T, kWide>;
   using Part = Vec<T, kPart>;
@@ -170,7 +170,8 @@ __global__ __launch_bounds__(kThreads, Dim == 256 || (Dim == 128 && Tiles == 2 &
   const T *const q0 = reinterpret_cast<const T *>(a.q);
   // 16 bits: m is half a product of q and k until the piece is written, and `by` takes differences of such halves to powers of 2.  A difference is taken
   // first, so that the largest key's is 0 whatever its product is: the rounding of a large product times `by` would be many powers of 2.  The
-  // difference of two products need not be a finite number of 32 bits where its power of 2 is; that of their halves is one.
+  // difference of two products need not be a finite number of 32 bits where its power of 2 is; that of their halves is one.  An instruction a score more than
+  // products times `by` less the maximum's: 64 requests behind 32768 keys 125.7 us and 124.1.
   constexpr float kOfProduct = sizeof(T) == 4 ? 1.0f : 0.5f;
   const float by = sizeof(T) == 4 ? 1.0f : a.scale == 0.0f ? 1.0f : fabsf(a.scale) * (kLog2e / kOfProduct);
   auto power = [by](float x) { return sizeof(T) == 4 ? exp_of(x) : __builtin_amdgcn_exp2f(x * by); };
@@ -458,8 +459,12 @@ template <class T, int Dim, int ColumnWaves, int Tiles> Variant variant() {
 }
 // As many columns as groups have on average: what is left empty costs as much as what is not, and more columns read the prefix less often.  16 instead of 32:
 // 6 requests of a head a key head (f32) 26.5 us and 35, 4 of four (f16) 6.4 and 7.5.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
-//   8 of 32 columns 41 / 40 / 48 (bf16), 82 / 114 / 178 (f32);  8 of 64 62 / 43 / 50, 143 / 119 / 183;  8 of 128 108 / 68 / 58, 267 / 223 / 195
-// The largest heads leave no registers for waves of other keys.
+//   8 of 32 columns 42 / 40 / 50 (bf16), 81 / 113 / 179 (f32);  8 of 64 63 / 43 / 51, 143 / 117 / 183;  8 of 128 108 / 68 / 60, 266 / 220 / 195
+// The average is over all requests and all places for groups, since which of them are in use is only known on the device.  Where most requests have no group it is too
+// large: one prefix of 4096 keys, 8 readers of four heads a key head, 38 us where they are the batch and 56 among 256 requests (bf16), 43.5 and 51.5 (f32).  Where
+// most places hold no group it is too small: 64 readers, 1 / 4 / 16 / 64 places 44.5 / 34 / 47 / 47 us (bf16), 65 / 67 / 94 / 94 (f32).
+// Heads of more than 128 elements of 16 bits have 128 columns however few are in use.  One group, 4096 keys, 8 key heads of 256 (bf16), us with 128 / 64 / 32 / 16 columns:
+//   16 in use 63 / 60 / 59 / 62;  32 65 / 61 / 60 / 46;  64 66 / 62 / 46 / 44;  128 68 / 50 / 46 / 57
 template <class T, int Dim> Variant variant_of_heads(unsigned columns) {
   constexpr int kMost = sizeof(T) == 4 && Dim == 256 ? 1 : 2;                  // tiles that the registers hold
   if constexpr (Dim < 256) {
