@@ -461,7 +461,7 @@ template <class T, int Dim, int ColumnWaves, int Tiles> Variant variant() {
 // 6 requests of a head a key head (f32) 26.5 us and 35, 4 of four (f16) 6.4 and 7.5.  Groups of 4096 keys, 8 key heads of 128, us with 32 / 64 / 128 columns:
 //   8 of 32 columns 42 / 40 / 50 (bf16), 81 / 113 / 179 (f32);  8 of 64 63 / 43 / 51, 143 / 117 / 183;  8 of 128 108 / 68 / 60, 266 / 220 / 195
 // The average is over all requests and all places for groups, since which of them are in use is only known on the device.  Where most requests have no group it is too
-// large: one prefix of 4096 keys, 8 readers of four heads a key head, 38 us where they are the batch and 56 among 256 requests (bf16), 43.5 and 51.5 (f32).  Where
+// large: one prefix of 4096 keys, 8 readers of four heads a key head, 38 us where they are the batch and 56 among 256 requests, whose rows are written too (bf16), 43.5 and 51.5 (f32).  Where
 // most places hold no group it is too small: 64 readers, 1 / 4 / 16 / 64 places 44.5 / 34 / 47 / 47 us (bf16), 65 / 67 / 94 / 94 (f32).
 // Heads of more than 128 elements of 16 bits have 128 columns however few are in use.  One group, 4096 keys, 8 key heads of 256 (bf16), us with 128 / 64 / 32 / 16 columns:
 //   16 in use 63 / 60 / 59 / 62;  32 65 / 61 / 60 / 46;  64 66 / 62 / 46 / 44;  128 68 / 50 / 46 / 57
